@@ -420,10 +420,10 @@ def _float_code(t, what):
     code = _FLOAT_CODES.get(t.dtype)
     if code is None:
         import torch
-        if not _FLOAT_CODES:
-            _FLOAT_CODES.update({torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16})
-            return _float_code(t, what)
-        raise TypeError("%s must be float32, bfloat16 or float16" % what)
+        _FLOAT_CODES.update({torch.float32: FLOAT32, torch.bfloat16: BFLOAT16, torch.float16: FLOAT16})
+        code = _FLOAT_CODES.get(t.dtype)        # another thread may have filled the table since the first look
+        if code is None:
+            raise TypeError("%s must be float32, bfloat16 or float16" % what)
     return code
 
 
@@ -435,8 +435,8 @@ def _stream_of(x):
     global _torch
     if _torch is None:
         import torch
-        _torch = torch
         lib()
+        _torch = torch      # last: the tensor forms use _lib without asking once this is set
     device = x.get_device()
     if device < 0 or not x.is_cuda or device != _torch._C._cuda_getDevice():
         raise ValueError("tensors must live on the current CUDA device")
