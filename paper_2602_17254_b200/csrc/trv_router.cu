@@ -449,7 +449,7 @@ __global__ void __launch_bounds__(kRtThreads, V == 8 && G >= 8 ? 4 : 1) k_router
 #pragma unroll
             for (int i = 0; i < TURNS; ++i) {
                 id[i] = (unsigned)next_id[i] < (unsigned)E ? next_id[i] : -1;
-                g[i] = next_g[i];
+                g[i] = id[i] >= 0 ? next_g[i] : 0.0f;       // what stands at a place that is not an expert may be NaN or infinite
                 w[i] = a.normalize && id[i] >= 0 ? to_f32(a.logits[t * a.ls + id[i]]) : -INFINITY;
             }
         fetch(t + step);

@@ -168,6 +168,21 @@ def test_ids_outside_the_experts_are_skipped():
         assert float((got.double().cpu() - want).abs().max()) <= 1e-5 * float(dg.abs().max())      # about 100 U times the largest summand
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("experts,k", [(6, 5), (40, 12), (81, 3), (256, 8), (600, 8)])
+def test_gates_gradients_without_an_expert_count_for_nothing(experts, k, dtype):
+    """NaN and infinities where a token has fewer open experts than choices, or is left out."""
+    logits, mask, dg = _logits(60, experts, dtype, 15, closed=1 - 1.5 * k / (experts + k))
+    dg = dg[:, :k].contiguous()
+    for normalize in (False, True):
+        ids, _, counts, _ = binding.router_forward_tensor(logits, k, mask, normalize)
+        none = ids < 0
+        assert bool((none & (ids[:, :1] >= 0)).any())                                # tokens with some choices but not all
+        for bad in (float("nan"), float("inf"), -float("inf")):
+            got = binding.router_backward_tensor(logits, ids, counts, COEF, torch.where(none, bad, dg), mask, normalize)
+            assert torch.equal(got, binding.router_backward_tensor(logits, ids, counts, COEF, torch.where(none, 0.0, dg), mask, normalize))
+
+
 @pytest.mark.parametrize("normalize", [False, True])
 def test_gradient_against_differences(normalize):
     """Central differences of the 64-bit loss + sum(w gates) with the counts and the choice held fixed."""
