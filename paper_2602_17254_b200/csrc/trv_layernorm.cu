@@ -410,8 +410,14 @@ __global__ void __launch_bounds__(SHARE == LN_WARP ? kLnThreads : kLnMaxThreads)
         Row::unpack(raw, d, de);
         small(r + step);
 #pragma unroll
-        for (int i = 0; i < P; ++i) {       // places outside the row have dy = gamma = 0 and add nothing
-            h[i] = f2_mul(f2_add(h[i], f2_splat(-mu)), f2_splat(rs));
+        for (int v = 0; v < Row::NP; ++v) {
+            // places outside the row have x = dy = gamma = 0 and add nothing: h = 0 there, for -mean rstd may overflow and 0 inf is NaN
+            const float2 m = VEC > 1 ? f2_splat(k.has(2 * Row::VP * v) ? -mu : 0.0f) : make_float2(k.has(2 * v) ? -mu : 0.0f, k.has(2 * v + 1) ? -mu : 0.0f);
+#pragma unroll
+            for (int i = v * Row::VP; i < (v + 1) * Row::VP; ++i) h[i] = f2_mul(f2_add(h[i], m), f2_splat(rs));
+        }
+#pragma unroll
+        for (int i = 0; i < P; ++i) {
             dg[i] = f2_fma(d[i], h[i], dg[i]);
             db[i] = f2_add(db[i], d[i]);
             d[i] = f2_mul(d[i], gm[i]);
@@ -420,7 +426,7 @@ __global__ void __launch_bounds__(SHARE == LN_WARP ? kLnThreads : kLnMaxThreads)
         }
         float s0 = t0.x + t0.y, s1 = t1.x + t1.y;
         if (EDGE) {
-            he = (he - mu) * rs;
+            he = k.has_edge() ? (he - mu) * rs : 0.0f;
             dge = fmaf(de, he, dge);
             dbe += de;
             de *= gme;

@@ -135,6 +135,23 @@ def test_nan_and_infinity_stay_in_their_rows():
     assert bool(dx[keep].isfinite().all()) and bool(dx[1].isnan().all())
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("cols", [3, 16, 100, 300, 1000, 2187, 4100, 9001, 12000])
+def test_level_times_rstd_beyond_binary32(cols, dtype):
+    """Constant rows far from zero: mean rstd overflows, every (x - mean) rstd is 0.  Places behind a row's end must not turn that into NaN."""
+    _, dy, gamma, _ = _inputs(11, cols, dtype, 16)
+    x = torch.full((11, cols), 2.0 ** 110, device=DEV).to(dtype)
+    mean, rstd = torch.full((11,), 2.0 ** 110, device=DEV), torch.full((11,), 2.0 ** 20, device=DEV)
+    dx, _, _ = _check_backward(dy, x, mean, rstd, gamma)
+    assert bool(dx.isfinite().all())
+    wide = torch.full((11, cols + 5), 2.0 ** 110, device=DEV).to(dtype)[:, 2:2 + cols]          # rows off 16-byte boundaries, dx and dy on them
+    dx, _, _ = _check_backward(dy, wide, mean, rstd, gamma)
+    assert bool(dx.isfinite().all())
+    x = torch.full((11, 64), 2.0 ** 120, device=DEV).to(dtype)                                   # and through the forward pass
+    _, mean, rstd = _check_forward(x, None, None, 1e-5)
+    _check_backward(dy.repeat(1, 22)[:, :64].contiguous(), x, mean, rstd, None)
+
+
 def test_no_rows():
     x = torch.empty(0, 100, device=DEV)
     y, mean, rstd = binding.layernorm_forward_tensor(x)
