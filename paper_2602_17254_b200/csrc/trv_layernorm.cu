@@ -544,16 +544,17 @@ __global__ void __launch_bounds__(1024) k_ln_bwd_sum(const float* __restrict__ p
     }
 }
 
-// CTAs of a kernel that an SM holds, asked once per kernel and CTA size
+// CTAs of a kernel that an SM holds; the last answer for a CTA size is kept with the shared memory it was given for (which goes by the
+// columns as well), so that grid and order of sums never depend on the widths of earlier calls
 template <typename K>
-static int ln_resident(K kernel, int threads, int smem, std::atomic<int>* cache) {
+static int ln_resident(K kernel, int threads, int smem, std::atomic<uint64_t>* cache) {
     // 48 KB are allowed without asking, the static arrays included; one size for all calls, so that none takes back another's
     if (smem > 32 << 10) allow_big_smem(kernel, 200 << 10);
-    int n = cache[threads / 32].load(std::memory_order_relaxed);
-    if (n == 0) {
-        if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
-        cache[threads / 32].store(n, std::memory_order_relaxed);
-    }
+    const uint64_t kept = cache[threads / 32].load(std::memory_order_relaxed);
+    if (kept && (int)(kept >> 32) == smem) return (int)(unsigned)kept;
+    int n = 0;
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, kernel, threads, smem) != cudaSuccess || n < 1) n = 1;
+    cache[threads / 32].store((uint64_t)smem << 32 | (unsigned)n, std::memory_order_relaxed);
     return n;
 }
 
@@ -570,7 +571,7 @@ static int ln_grid(long long rows, int resident) {
 
 template <typename T, int VEC, int NV, bool EDGE, bool WARP, int AHEAD, bool MANY = false>
 static void ln_fwd_launch(const LnFwd<T>& a, cudaStream_t st) {
-    static std::atomic<int> cache[33];
+    static std::atomic<uint64_t> cache[33];
     const int threads = ln_threads<VEC, NV, WARP>(a.cols);
     const int smem = VEC > 1 ? LnRow<T, VEC, NV, EDGE, AHEAD>::D * NV * 16 * threads : 0;
     const int resident = ln_resident(k_ln_fwd<T, VEC, NV, EDGE, WARP, AHEAD, MANY>, threads, smem, cache);
@@ -606,7 +607,7 @@ static void ln_forward(const LnFwd<T>& a, cudaStream_t st) {
 
 template <typename T, int VEC, int NV, bool EDGE, LnShare SHARE>
 static int ln_bwd_launch(LnBwd<T> a, cudaStream_t st) {
-    static std::atomic<int> cache[33];
+    static std::atomic<uint64_t> cache[33];
     constexpr bool WARP = SHARE == LN_WARP, PAIR = SHARE == LN_PAIR;
     int cols = a.cols;
     if (PAIR) cols = a.cols0 = (a.cols + 2 * VEC - 1) / (2 * VEC) * VEC;        // the larger half

@@ -1,4 +1,8 @@
 """Layer norm forward and backward against plain 64-bit forms, and the backward pass against differences."""
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
@@ -197,6 +201,26 @@ def test_same_bits_every_time_and_on_other_streams():
     torch.cuda.synchronize()
     for f, b in got:
         assert torch.equal(f[0], y0) and all(torch.equal(p, q) for p, q in zip(b, b0))
+
+
+def test_the_bits_do_not_depend_on_the_widths_of_earlier_calls():
+    """Two fresh processes, the same widths in opposite orders; many of them share a CTA size with others."""
+    code = """
+import hashlib, sys, torch
+from paper_2602_17254_b200 import binding
+for dtype in (torch.bfloat16, torch.float32):
+    for cols in sorted((40, 100, 250, 300, 500, 600, 700, 1000, 1500, 2000, 2187, 3000, 4096), reverse=sys.argv[1] == "down"):
+        g = torch.Generator(device="cuda").manual_seed(cols)
+        x = torch.randn(4000, cols, device="cuda", generator=g).to(dtype)
+        dy = torch.randn(4000, cols, device="cuda", generator=g).to(dtype)
+        y, mean, rstd = binding.layernorm_forward_tensor(x)
+        parts = (y, *binding.layernorm_backward_tensor(dy, x, mean, rstd))
+        print(dtype, cols, hashlib.sha256(b"".join(t.float().cpu().numpy().tobytes() for t in parts)).hexdigest())
+"""
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    lines = [subprocess.run([sys.executable, "-c", code, order], cwd=root, capture_output=True, text=True, timeout=300, check=True).stdout.splitlines()
+             for order in ("up", "down")]
+    assert len(lines[0]) == 26 and sorted(lines[0]) == sorted(lines[1])
 
 
 def test_inside_a_graph():
