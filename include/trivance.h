@@ -363,7 +363,8 @@ trv_status_t trv_cost_model(trv_plan_t plan, size_t count, size_t elem_size, dou
  * cuda_stream, allocate nothing, work on the current device and may run on any number of streams and threads at once as long as
  * their outputs and workspaces differ.  Matrices are row-major with unit inner stride and a row stride in ELEMENTS; rows may be
  * aligned to their element size only (16-byte aligned rows of equal 16-byte offsets are faster).  A size of zero is no error.
- * Outputs and workspaces must not overlap inputs or one another (INVALID_ARG).  Sums, statistics and softmaxes are binary32 or
+ * Outputs and workspaces must not overlap inputs or one another (INVALID_ARG); column slices of one buffer that share no element
+ * are fine.  Sums, statistics and softmaxes are binary32 or
  * wider; every result is rounded once, to the type of its buffer, and is the same from run to run (no floating atomics).
  * workspace: DEVICE, 256-byte aligned, at least the bytes the query names (SCRATCH otherwise); contents undefined before and after.
  *

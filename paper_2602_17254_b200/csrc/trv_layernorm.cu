@@ -688,8 +688,8 @@ extern "C" trv_status_t trv_layernorm_forward(const void* x, const void* gamma, 
     const size_t es = dtype_bytes(dtype), ps = dtype_bytes(param_dtype);
     if (misaligned(x, es) || misaligned(y, es) || misaligned(gamma, ps) || misaligned(beta, ps) || misaligned(mean, 4) || misaligned(rstd, 4))
         return TRV_ERR_INVALID_ARG;
-    const Span in[3] = {{x, matrix_bytes(rows, cols, x_stride, es)}, {gamma, cols * ps}, {beta, cols * ps}};
-    const Span out[3] = {{y, matrix_bytes(rows, cols, y_stride, es)}, {mean, rows * 4}, {rstd, rows * 4}};
+    const Span in[3] = {matrix_span(x, rows, cols, x_stride, es), {gamma, cols * ps}, {beta, cols * ps}};
+    const Span out[3] = {matrix_span(y, rows, cols, y_stride, es), {mean, rows * 4}, {rstd, rows * 4}};
     if (!disjoint(in, out)) return TRV_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     auto run = [&](auto zero) {
@@ -731,9 +731,9 @@ extern "C" trv_status_t trv_layernorm_backward(const void* dy, const void* x, co
         trv_layernorm_workspace_bytes(rows, cols, &need);
         if (!workspace || misaligned(workspace, 256) || workspace_bytes < need) return TRV_ERR_SCRATCH;
     }
-    const Span in[5] = {{dy, matrix_bytes(rows, cols, dy_stride, es)}, {x, matrix_bytes(rows, cols, x_stride, es)}, {gamma, cols * ps},
+    const Span in[5] = {matrix_span(dy, rows, cols, dy_stride, es), matrix_span(x, rows, cols, x_stride, es), {gamma, cols * ps},
                         {mean, rows * 4}, {rstd, rows * 4}};
-    const Span out[4] = {{dx, matrix_bytes(rows, cols, dx_stride, es)}, {dgamma, cols * 4}, {dbeta, cols * 4}, {workspace, need}};
+    const Span out[4] = {matrix_span(dx, rows, cols, dx_stride, es), {dgamma, cols * 4}, {dbeta, cols * 4}, {workspace, need}};
     if (!disjoint(in, out)) return TRV_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     auto run = [&](auto zero) {

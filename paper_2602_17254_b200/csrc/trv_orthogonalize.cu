@@ -1182,8 +1182,13 @@ extern "C" trv_status_t trv_orthogonalize(const void* g, void* out, size_t batch
     const NsLayout L = ns_layout(batch, rows, cols);
     const size_t need = ns_is_small(L) ? 0 : L.bytes;
     if (need && (!workspace || misaligned(workspace, 256) || workspace_bytes < need)) return TRV_ERR_SCRATCH;
-    const Span in[1] = {{g, ((batch - 1) * g_batch_stride + (rows - 1) * g_stride + cols) * es}};
-    const Span outs[2] = {{out, ((batch - 1) * out_batch_stride + (rows - 1) * out_stride + cols) * 2}, {workspace, need}};
+    // a batch of matrices is one matrix of their rows if the distance between them is a whole number of rows
+    auto span = [&](const void* p, size_t stride, size_t batch_stride, size_t size) {
+        const bool whole = batch == 1 || batch_stride % stride == 0;
+        return Span{p, ((batch - 1) * batch_stride + (rows - 1) * stride + cols) * size, cols * size, whole ? stride * size : 0};
+    };
+    const Span in[1] = {span(g, g_stride, g_batch_stride, es)};
+    const Span outs[2] = {span(out, out_stride, out_batch_stride, 2), {workspace, need}};
     if (!disjoint(in, outs)) return TRV_ERR_INVALID_ARG;
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     unsigned char* ws = (unsigned char*)workspace;

@@ -589,7 +589,7 @@ extern "C" trv_status_t trv_router_forward(const void* logits, const uint8_t* ma
     size_t need = 0;
     trv_router_workspace_bytes(tokens, experts, &need);
     if (need && (!workspace || misaligned(workspace, 256) || workspace_bytes < need)) return TRV_ERR_SCRATCH;
-    const Span in[2] = {{logits, matrix_bytes(tokens, E, logits_stride, es)}, {mask, tokens}};
+    const Span in[2] = {matrix_span(logits, tokens, E, logits_stride, es), {mask, tokens}};
     const Span out[5] = {{ids, picks}, {gates, picks}, {counts, (E + 1) * 4}, {prob_sum, E * 4}, {workspace, need}};
     if (!disjoint(in, out)) return TRV_ERR_INVALID_ARG;
     const int blocks = rt_blocks(tokens, experts);
@@ -637,9 +637,9 @@ extern "C" trv_status_t trv_router_backward(const void* logits, const uint8_t* m
     const size_t es = dtype_bytes(dtype), E = (size_t)experts, picks = tokens * (size_t)top_k * 4;
     if (misaligned(logits, es) || misaligned(dlogits, es) || misaligned(ids, 4) || misaligned(dgates, 4) || misaligned(counts, 4))
         return TRV_ERR_INVALID_ARG;
-    const Span in[5] = {{logits, matrix_bytes(tokens, E, logits_stride, es)}, {mask, tokens}, {ids, dgates ? picks : 0}, {dgates, picks},
+    const Span in[5] = {matrix_span(logits, tokens, E, logits_stride, es), {mask, tokens}, {ids, dgates ? picks : 0}, {dgates, picks},
                         {counts, (E + 1) * 4}};
-    const Span out[1] = {{dlogits, matrix_bytes(tokens, E, dlogits_stride, es)}};
+    const Span out[1] = {matrix_span(dlogits, tokens, E, dlogits_stride, es)};
     if (!disjoint(in, out)) return TRV_ERR_INVALID_ARG;
     auto run = [&](auto zero) {
         RouterArgs<decltype(zero)> a = {};

@@ -64,14 +64,24 @@ inline size_t dtype_bytes(trv_dtype_t t) { return t == TRV_BFLOAT16 || t == TRV_
 inline bool float_dtype(trv_dtype_t t) { return t == TRV_FLOAT32 || t == TRV_BFLOAT16 || t == TRV_FLOAT16; }
 // bytes from the first to behind the last element of a strided matrix
 inline size_t matrix_bytes(size_t rows, size_t cols, size_t stride, size_t es) { return rows ? ((rows - 1) * stride + cols) * es : 0; }
+// Memory of an operand: `bytes` from p on; a matrix also says which of them are its own, `row` of every `stride` bytes
 struct Span {
     const void* p;
-    size_t bytes;
+    size_t bytes, row, stride;
 };
+inline Span matrix_span(const void* p, size_t rows, size_t cols, size_t stride, size_t es) {
+    return {p, matrix_bytes(rows, cols, stride, es), cols * es, stride * es};
+}
 inline bool meet(const Span& a, const Span& b) {
     if (!a.p || !b.p || !a.bytes || !b.bytes) return false;
     const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-    return x < y + b.bytes && y < x + a.bytes;
+    if (x >= y + b.bytes || y >= x + a.bytes) return false;
+    // column slices of one buffer: equal strides, and b's columns behind a's and before a's next row
+    if (a.stride && a.stride == b.stride) {
+        const size_t off = y >= x ? (y - x) % a.stride : (a.stride - (x - y) % a.stride) % a.stride;
+        return off < a.row || off + b.row > a.stride;
+    }
+    return true;
 }
 // no output may touch an input or another output
 template <int NI, int NO>
