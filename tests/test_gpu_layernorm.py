@@ -103,6 +103,33 @@ def test_strides_and_offsets(cols, pad, shift, dtype):
     assert bool((frame[:, :shift] == 7).all()) and bool((frame[:, shift + cols:] == 7).all())
 
 
+def _view(t, pad, shift):
+    """t's values as a view into a wider matrix of sevens; and that matrix."""
+    frame = torch.full((t.shape[0], t.shape[1] + pad + shift), 7.0, dtype=t.dtype, device=DEV)
+    view = frame[:, shift:shift + t.shape[1]]
+    view.copy_(t)
+    return view, frame
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,cols", [(23, 9), (23, 33), (50, 100), (23, 257), (23, 1000), (40, 2047), (23, 4096), (23, 4097), (11, 9000), (5, 16384),
+                                       (5, 20000), (20001, 60), (3001, 500), (2501, 1000), (1301, 3000), (1201, 4096), (700, 5000)])
+@pytest.mark.parametrize("mixed", [0, 1])
+def test_every_operand_with_a_stride_and_an_offset_of_its_own(rows, cols, dtype, mixed):
+    """Rows that start at different places of a 16-byte vector in x, dy and the results, several rows to a CTA among them; nothing
+    outside the results is written.  mixed = 0: only x is a view, the results are contiguous."""
+    x, dy, gamma, beta = _inputs(rows, cols, dtype, 17)
+    x, _ = _view(x, 3, 1)
+    y, yf = _view(torch.zeros_like(dy), 5, 2) if mixed else (None, None)
+    dx, dxf = _view(torch.zeros_like(dy), 9, 4) if mixed else (None, None)
+    if mixed:
+        dy, _ = _view(dy, 2, 0)
+    _, mean, rstd = _check_forward(x, gamma, beta, 1e-5, out=y)
+    _check_backward(dy, x, mean, rstd, gamma, out=dx)
+    for view, frame, shift in ((y, yf, 2), (dx, dxf, 4)) if mixed else ():
+        assert bool((frame[:, :shift] == 7).all()) and bool((frame[:, shift + cols:] == 7).all())
+
+
 def test_parameters_at_odd_addresses():
     x, dy, gamma, beta = _inputs(12, 513, torch.float32, 6)
     x, dy = x[:, :512].contiguous(), dy[:, :512].contiguous()
