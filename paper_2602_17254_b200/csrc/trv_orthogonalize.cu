@@ -316,6 +316,12 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
     }
 }
 
+// The last copies of a CTA that issued n stages (full barriers at bar, parity flips per turn) have landed: no CTA leaves with a copy
+// on its way, not even after a wait that ran out.
+__device__ __forceinline__ void ns_landed(unsigned bar, unsigned n) {
+    for (unsigned k = n > kNsMaxStages ? n - kNsMaxStages : 0; k < n; ++k) ns_wait(bar + 8 * (k % kNsMaxStages), k / kNsMaxStages & 1);
+}
+
 // One 128 x 128 tile of  left . right  per cluster, the sum over K split over its CTAs.  left: rows along y, K along x.
 // right: the same (GRAM, POLY: the product with its transpose) or rows of K, N along x (APPLY, LAST).  Bound by latency: a launch
 // is filling the stages from L2, K / 64 blocks of products, the exchange of a split and one epilogue.  512 x 512: 107 us for 15
@@ -326,7 +332,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
                                                            const __grid_constant__ NsArgs a, int split) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kNsMaxStages + 1];
+    __shared__ __align__(8) unsigned long long bars[2 * kNsMaxStages + 2];
     __shared__ unsigned tmem_at;
     const int warp = ns_warp(), lane = threadIdx.x & 31, part = blockIdx.x % split, tj = blockIdx.x / split, ti = blockIdx.y, z = blockIdx.z;
     pdl_trigger();
@@ -334,13 +340,13 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
     const unsigned base = (smem_u32(raw) + 1023) & ~1023u, bar = smem_u32(bars);
     auto full = [&](int s) { return bar + 8 * s; };
     auto empty = [&](int s) { return bar + 8 * (kNsMaxStages + s); };
-    const unsigned done = bar + 8 * 2 * kNsMaxStages;
+    const unsigned done = bar + 8 * 2 * kNsMaxStages, left_off = done + 8;
     if (threadIdx.x == 32 * kNsEpilogueWarps) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
     }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < 2 * kNsMaxStages + 1; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
+        for (int s = 0; s < 2 * kNsMaxStages + 2; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -361,7 +367,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
     pdl_wait();
     if (warp == kNsEpilogueWarps) {
         if (lane == 0) {
-            for (int k = 0, s = 0, ph = 1; k < nk; ++k) {
+            int k = 0;
+            for (int s = 0, ph = 1; k < nk; ++k) {
                 if (!(ok = ns_wait(empty(s), ph))) break;
                 const unsigned dst = base + s * kNsStageBytes;
                 const int x = (k0 + k) * kNsK;
@@ -375,6 +382,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
                 }
                 if (++s == kNsMaxStages) s = 0, ph ^= 1;
             }
+            ns_landed(bar, k);
         }
     } else if (warp == kNsEpilogueWarps + 1) {
         for (int k = 0, s = 0, ph = 0; k < nk; ++k) {
@@ -385,7 +393,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
             ns_commit<1>(empty(s));
             if (++s == kNsMaxStages) s = 0, ph ^= 1;
         }
-        if (ok) ns_commit<1>(done);
+        ns_commit<1>(ok ? done : left_off);
+        if (!ok) ns_wait(left_off, 0);                      // its products too
     } else {
         if (cols) ns_fetch<MODE>(a, z, i0 + 32 * q, j0 + first, mine);
         ok = __all_sync(~0u, ns_wait(done, 0));
@@ -478,7 +487,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
                                                                                      const __grid_constant__ NsArgs a) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     extern __shared__ unsigned char raw[];
-    __shared__ __align__(8) unsigned long long bars[2 * kNsMaxStages + 4];
+    __shared__ __align__(8) unsigned long long bars[2 * kNsMaxStages + 5];
     __shared__ unsigned tmem_at;
     const int warp = ns_warp(), lane = threadIdx.x & 31;
     const unsigned rank = ns_cluster_rank();
@@ -488,13 +497,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
     auto empty = [&](int s) { return bar + 8 * (kNsMaxStages + s); };           // each CTA's: the products have read the stage
     auto sums = [&](int t) { return bar + 8 * (2 * kNsMaxStages + t); };        // each CTA's: the sums of a tile are complete
     auto taken = [&](int t) { return bar + 8 * (2 * kNsMaxStages + 2 + t); };   // CTA 0's: both CTAs' epilogue warps have read them
+    const unsigned left_off = bar + 8 * (2 * kNsMaxStages + 4);                 // each CTA's: products issued before a wait ran out
     if (threadIdx.x == 32 * kNsEpilogueWarps) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
     }
     if (threadIdx.x == 0) {
-        for (int s = 0; s < 2 * kNsMaxStages + 4; ++s)
-            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar + 8 * s), "r"(s < 2 * kNsMaxStages + 2 ? 1 : 2 * kNsEpilogueWarps) : "memory");
+        for (int s = 0; s < 2 * kNsMaxStages + 5; ++s)
+            asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;"
+                         ::"r"(bar + 8 * s), "r"(s == 2 * kNsMaxStages + 2 || s == 2 * kNsMaxStages + 3 ? 2 * kNsEpilogueWarps : 1) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
     }
@@ -514,6 +525,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
     pdl_wait();
     if (warp == kNsEpilogueWarps) {
         if (lane == 0) {
+            unsigned loads = 0;
             for (int s = 0, ph = 1, n = pair; n < a.tiles && ok; n += pairs) {
                 int ti, tj, z;
                 ns_tile_at<kSym>(a, n, &z, &ti, &tj);
@@ -529,9 +541,11 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
                         ns_load<2>(dst + kNsHalf, &right, j0, k * kNsK, z, at);
                         ns_load<2>(dst + kNsHalf + 8192, &right, j0 + 64, k * kNsK, z, at);
                     }
+                    ++loads;
                     if (++s == kNsMaxStages) s = 0, ph ^= 1;
                 }
             }
+            if (rank == 0) ns_landed(bar, loads);           // both CTAs' copies; the other CTA waits for this one before it leaves
         }
     } else if (warp == kNsEpilogueWarps + 1) {
         if (rank == 0) {
@@ -550,6 +564,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
                 if (ok) ns_commit<2>(sums(t));
                 if (++t == 2) t = 0, tph ^= 1;
             }
+            if (!ok) ns_commit<2>(left_off), ns_wait(left_off, 0);
         }
     } else {
         const int q = warp & 3, first = 64 * (warp >> 2);
