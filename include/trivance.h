@@ -419,11 +419,13 @@ trv_status_t trv_router_backward(const void *logits, const uint8_t *mask, const 
 /* Orthogonalises a batch of update matrices by Newton-Schulz products: X = G / (|G|_F + eps), transposed if G is taller than wide;
  * `steps` times A = X X^T, X <- a X + (b A + c A A) X; the result is X in G's orientation.
  *   g            : DEVICE [batch][rows][cols] of dtype (FLOAT32, BFLOAT16, FLOAT16); strides in elements (rows, matrices)
- *   out          : DEVICE BFLOAT16, same shape, strides of its own; its matrices must not overlap.  The products run on binary16
- *                  operands with binary32 sums (diagonals and the carried term in more bits): about 0.1 % (2-norm) from the exact
- *                  result, which is less than BFLOAT16's own rounding.  The order of the sums goes by the sizes, the batch included
- *   coefficients : HOST float [steps][3] = (a, b, c) of every step, NULL: 3.4445, -4.7750, 2.0315 in all.  b A + c A A must stay
- *                  below 255 in magnitude (singular values stay below about 1.3 with the default), else the result is infinite or NaN
+ *   out          : DEVICE BFLOAT16, same shape, strides of its own; its matrices must not overlap.  Products of binary16
+ *                  operands with binary32 sums.  With one side of at most 128 and the other of at most 4096 operands have two binary16
+ *                  halves: within 0.05 % (2-norm) of the exact result before its rounding to BFLOAT16 (0.17 %), for every spectrum.
+ *                  Else one half (diagonals and the carried term in more bits): about 0.1 % where no direction stands out.
+ *                  The order of the sums goes by the sizes, the batch included
+ *   coefficients : HOST float [steps][3] = (a, b, c) of every step, NULL: 3.4445, -4.7750, 2.0315 in all.  A and a I + b A + c A A must
+ *                  stay below 255 in magnitude (singular values stay below about 1.3 with the default), else the result is infinite or NaN
  * A zero matrix gives zeros.  Limits: steps 1 .. 64 (INVALID_ARG), rows and cols 2^20, batch 65535 (UNSUPPORTED).
  * The first call on a device looks up a device address and the tensor-map encoder: make it outside any stream capture.
  * Bounded waits as in the other copy-engine kernels: see trv_tma_giveups. */

@@ -3,15 +3,18 @@
 //     A = X X^T,   B = b A + c A A,   X <- a X + B X
 // and the result is X.  The three products run on the tensor cores (tcgen05, binary16 operands, binary32 sums in tensor memory).
 //
-// Number formats.  X is held as hi + lo, two binary16 numbers (22 bits): hi is the operand of the products, the carried term a X
-// uses both.  A gradient has a few strong directions and many weak ones; the weak ones grow by a factor of up to a in every step,
-// and so would the rounding of the strong ones that falls on them.  A and B are nearly diagonal once the singular values are near
-// 1, so their diagonals are kept apart, in binary32, and only the rest is rounded to binary16:
+// Number formats.  A gradient has a few strong directions and many weak ones; the weak ones grow by a factor of up to a in every
+// step, and so does every rounding of the strong ones that falls on them.  So X is held as hi + lo, two binary16 numbers (22 bits).
+// On chip (k_ns_small: a side of at most 128, the other up to 4096) all three products take both halves of both operands, hi lo +
+// lo hi + hi hi; B includes a I.  The result is then within 0.05 % of the 64-bit one for every spectrum and for steep
+// coefficients, 0.01 % mostly.
+// In the tiled kernels hi alone is the operand and the carried term a X uses both.  A and B are nearly diagonal once the singular
+// values are near 1, so their diagonals are kept apart, in binary32, and only the rest is rounded to binary16:
 //     A = D + O,  B = E + P:  P = b O + c (O O + (D_i + D_j) O) off the diagonal, E = b D + c (O O + D D) on it,
 //     X <- (a + E_i) X + P X,
-// which takes the diagonal's products out of the rounded operands.  The result is then within 0.04 - 0.1 % of the 64-bit one, for
-// noise and for low-rank inputs (diagonals inside A and B: 0.15 - 0.2 %; hi alone for the carried term: 2 - 7 % at low rank).
-// Scaling by powers of two keeps everything in binary16's normal range: X times sx ~ sqrt(N), A and B times 256.
+// which takes the diagonal's products out of the rounded operands.  The result is then within 0.04 - 0.1 % of the 64-bit one for
+// noise (diagonals inside A and B: 0.15 - 0.2 %; hi alone for the carried term: 2 - 7 % at low rank).
+// Scaling by powers of two keeps everything in binary16's normal range: X times sx ~ sqrt(N), A and B times 256, lo times 2^11.
 //
 // Products with 128 x 128 tiles, one CTA each (k_ns_tile); the sum over K may be split over a cluster of 2 or 4 CTAs, which add
 // their parts through distributed shared memory in a fixed order.  Large products with 256 x 256 tiles, two CTAs each
@@ -98,6 +101,18 @@ __device__ __forceinline__ void ns_mma(unsigned tmem, unsigned long long a, unsi
         asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.ne.s32 p, %4, 0;\n\t"
                      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                      ::"r"(tmem), "l"(a), "l"(b), "r"(idesc), "r"(add) : "memory");
+}
+// The same, and what was added up so far counts 2^-11 (the instruction's own scaling of the addend): products with a low half, which
+// is held times 2^11, come first, and the first one without begins like this.
+constexpr float kNsLow = 2048.0f;
+template <int CG>
+__device__ __forceinline__ void ns_mma_shift(unsigned tmem, unsigned long long a, unsigned long long b, unsigned idesc) {
+    if (CG == 1)
+        asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.eq.s32 p, 0, 0;\n\t"
+                     "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p, 11;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.eq.s32 p, 0, 0;\n\t"
+                     "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, 11;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc) : "memory");
 }
 // one stage: K = 64 in four products.  left: 128 rows of 128 bytes; right: the same, or (N_MAJOR) 64 rows of K for every 64 columns
 template <int CG, bool N_MAJOR>
@@ -598,13 +613,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
 }
 
 // Matrices with M <= 128, whole iterations on chip: one CTA, or a cluster of up to 16 that share the columns, per matrix; one launch
-// for a batch.  X lives in tensor memory in binary32 (times 256, so that B X adds onto it directly) and as binary16 in shared
-// memory, where one 128-byte-swizzled layout serves as K-major operand of X X^T and as N-major operand of B X; A and B live in
-// shared memory.  A step is three products and four passes over registers, 16 columns of a row per thread and turn; a cluster adds
-// the CTAs' parts of X X^T through distributed shared memory, every CTA a share of the columns, in a fixed order.  Bound by the
-// latency of this chain: 81 x 243 float32 31 us, 32 matrices of 128 x 1000 61 us (a third of a step is the cluster's sum), 16 x 40
-// 14 us.  Sides are rounded up to 16, not to 128: 16 x 40 took 24 us with 128.  The code is kept small (loops of 16 columns, one pass for every purpose): run once by a CTA it comes from
-// memory, and unrolled loads of 128 elements a thread took 20 us for their instructions alone.
+// for a batch.  X is in tensor memory in binary32 (times 256, as B X leaves it) and as two binary16 halves in shared memory, where one
+// 128-byte-swizzled layout serves as K-major operand of X X^T and as N-major operand of B X; A and B are there too.  A step is
+// three products (three times: see the header) and three passes over registers, 16 columns of a row per thread and turn; a cluster
+// adds the CTAs' parts of X X^T through distributed shared memory, every CTA a share of the columns, in a fixed order.  Bound by the
+// latency of this chain: 81 x 243 float32 43 us, 32 matrices of 128 x 1000 94 us, 16 x 40 16 us (with high halves alone 31, 61
+// and 14 us and errors of up to 3 %: 2/3 of the difference are the additional products, the rest of a cluster's the doubled exchange of A).
+// Sides are rounded up to 16, not to 128: 16 x 40 took 24 us with 128.  The code is kept small (loops of 16 columns, one pass for
+// every purpose): run once by a CTA it comes from memory, and unrolled loads of 128 elements a thread took 20 us for their
+// instructions alone.
 constexpr int kNsSmallThreads = 512, kNsSmallWidth = 256, kNsSmallCluster = 16;
 struct NsSmall {
     const void* g;
@@ -616,6 +633,10 @@ struct NsSmall {
     unsigned* giveups;
     float c[3 * 64];
 };
+
+// bytes of X's low half (or a cluster's parts of A: 128 x 128 binary32) and of a half of A
+__host__ __device__ constexpr int ns_small_low(int W, int C) { return C > 1 ? 65536 : W * 256; }
+__host__ __device__ constexpr int ns_small_square(int M) { return M > 64 ? 32768 : 16384; }
 
 __device__ __forceinline__ void ns_ld16(unsigned tmem, float (&v)[16]) {
     unsigned r[16];
@@ -674,30 +695,33 @@ __device__ __forceinline__ bool ns_poll(unsigned bar, unsigned parity) {
 }
 __device__ __forceinline__ void ns_wait_st() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void ns_fence_async() { asm volatile("fence.proxy.async;" ::: "memory"); }
-__device__ __forceinline__ uint4 ns_half8(const float* v, float s) {
-    unsigned u[4];
+// 8 values times s (a power of two) as binary16, and what that leaves out times 2^11 as binary16: 22 bits
+__device__ __forceinline__ void ns_split8(const float* v, float s, uint4& hi, uint4& lo) {
+    unsigned u[4], w[4];
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         const float2 f = f2_mul(make_float2(v[2 * k], v[2 * k + 1]), f2_splat(s));
         const __half2 h = __floats2half2_rn(f.x, f.y);
-        memcpy(&u[k], &h, 4);
+        const float2 r = f2_mul(f2_fma(__half22float2(h), f2_splat(-1.0f), f), f2_splat(kNsLow));
+        u[k] = ns_bits(h), w[k] = ns_bits(__floats2half2_rn(r.x, r.y));
     }
-    return make_uint4(u[0], u[1], u[2], u[3]);
+    hi = make_uint4(u[0], u[1], u[2], u[3]), lo = make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 template <typename T>
 __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_constant__ NsSmall a) {
     extern __shared__ unsigned char raw[];
     __shared__ __align__(8) unsigned long long bars[1];
-    __shared__ __align__(16) float D[128], E[128];          // diagonals of A and B
     __shared__ double part_norm[kNsSmallCluster], red[kNsSmallThreads / 32];
     __shared__ unsigned tmem_at;
     constexpr int kWarps = kNsSmallThreads / 32;
     const int t = threadIdx.x, warp = ns_warp(), lane = t & 31, quarter = warp >> 2, row = 32 * (warp & 3) + lane;
     const int rank = a.C > 1 ? (int)ns_cluster_rank() : 0, z = blockIdx.x / a.C, n0 = rank * a.W;
     const unsigned base = (smem_u32(raw) + 1023) & ~1023u, bar = smem_u32(bars);
-    const unsigned xh = base, ob = xh + a.W * 256, pb = ob + 32768, parts = pb + 32768;
-    // [128][W] words over X, A and B, before the first and after the last step; the columns of a row permuted by the row
+    // X, A and B as high and low halves.  B takes A's place (element by element); a cluster's parts of A take that of X's low half,
+    // which is then written again.
+    const unsigned xh = base, xl = xh + a.W * 256, sh = xl + ns_small_low(a.W, a.C), sl = sh + ns_small_square(a.M), parts = xl;
+    // [128][W] words over X, before the first and after the last step; the columns of a row permuted by the row
     float* stage = (float*)(raw + (base - smem_u32(raw)));
     auto unit = [&](unsigned at, int r, int u) { return at + (u >> 3) * 16384 + r * 128 + (((u & 7) ^ (r & 7)) << 4); };  // 8 columns of a row
     const int tcols = a.W <= 128 ? 256 : 512;
@@ -786,7 +810,7 @@ __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_const
 
     bool ok = true;
     unsigned phase = 0;
-    auto product = [&](auto issue) {                        // what all wrote is in place; warp 0 issues, all wait
+    auto product = [&](auto issue, auto meanwhile) {        // what all wrote is in place; warp 0 issues, all do the other and wait
         ns_fence_async();
         ns_fence_before();
         __syncthreads();
@@ -795,10 +819,35 @@ __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_const
             issue();
             ns_commit<1>(bar);
         }
+        meanwhile();
         if (!ns_poll(bar, phase)) ok = false;
         phase ^= 1;
         __syncwarp();
         ns_fence_after();
+    };
+    // Three products each: high . low, low . high, then high . high, over 16 columns of left k16 times (and of right, or rows of right).
+    // Unrolled by twelve: rolled products issue slower (81 x 243 61 us, by four 51, by twelve 49).  High halves alone in the last step
+    // save 2 us and cost 0.05 - 0.5 %.
+    auto three = [&](unsigned to, unsigned lh, unsigned ll, unsigned rh, unsigned rl, int k16, bool n_major, unsigned idesc) {
+#pragma unroll
+        for (int n = 0; n < 3; ++n) {
+            const unsigned l = n == 1 ? ll : lh, r = n == 0 ? rl : rh;
+#pragma unroll 1
+            for (int k = 0; k < k16; k += 4)
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const unsigned long long a = ns_desc(l + (k >> 2) * 16384 + q * 32, 16, 1024);
+                    const unsigned long long b = n_major ? ns_desc(r + (k + q) * 2048, 16384, 1024) : ns_desc(r + (k >> 2) * 16384 + q * 32, 16, 1024);
+                    if (q == 0 && n == 2 && k == 0) ns_mma_shift<1>(to, a, b, idesc);
+                    else if (k + q < k16) ns_mma<1>(to, a, b, idesc, n || k || q);
+                }
+        }
+    };
+    auto squares = [&](unsigned h, unsigned l, int k16) { three(ts, h, l, h, l, k16, false, ns_idesc(128, mp, false)); };
+    auto store = [&](unsigned h, unsigned l, int u, const float* v, float s) {
+        uint4 hi, lo;
+        ns_split8(v, s, hi, lo);
+        ns_sts(unit(h, row, u), hi), ns_sts(unit(l, row, u), lo);
     };
     const float to_a = kNsScale / (a.sx * a.sx);
 #pragma unroll 1
@@ -807,31 +856,20 @@ __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_const
         for (int c = x0; c < x1; c += 16) {
             float v[16];
             ns_ld16(tx + mine + c, v);
-            ns_sts(unit(xh, row, c / 8), ns_half8(v, 1.0f / kNsScale));
-            ns_sts(unit(xh, row, c / 8 + 1), ns_half8(v + 8, 1.0f / kNsScale));
+            store(xh, xl, c / 8, v, 1.0f / kNsScale);
+            store(xh, xl, c / 8 + 1, v + 8, 1.0f / kNsScale);
         }
-        product([&] {
-#pragma unroll 1
-            for (int k = 0; k < a.W / 64; ++k)
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const unsigned long long d = ns_desc(xh + k * 16384 + q * 32, 16, 1024);
-                    ns_mma<1>(ts, d, d, ns_idesc(128, mp, false), k | q);
-                }
-        });
+        product([&] { squares(xh, xl, a.W / 16); }, [] {});
         if (a.C == 1) {
 #pragma unroll 1
             for (int u = u0; u < u1; ++u) {
                 float v[8];
                 ns_ld8(ts + mine + 8 * u, v);
-                if (row >> 3 == u) {
-#pragma unroll
-                    for (int q = 0; q < 8; ++q)
-                        if (row == 8 * u + q) D[row] = v[q] * to_a, v[q] = 0;
-                }
-                ns_sts(unit(ob, row, u), ns_half8(v, to_a));
+                store(sh, sl, u, v, to_a);
             }
         } else {
+            ns_cluster_arrive();                            // all CTAs have read their low halves of X
+            ns_cluster_wait();
             // 8 columns of a row at a time to the CTA that adds them: [part][its units][half][128 rows] of 16 bytes
             const int own = (units + a.C - 1) / a.C;        // units of a CTA
 #pragma unroll 1
@@ -862,16 +900,14 @@ __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_const
 #pragma unroll
                     for (int q = 0; q < 8; ++q) v[q] += f[q];
                 }
-                float d = 0;
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (r == 8 * u + q) d = v[q] * to_a, v[q] = 0;
-                const uint4 w = ns_half8(v, to_a);
+                uint4 w[2];
+                ns_split8(v, to_a, w[0], w[1]);
 #pragma unroll 1
                 for (int p = 0; p < a.C; ++p) {
-                    asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ns_peer(unit(ob, r, u), p)), "r"(w.x), "r"(w.y), "r"(w.z), "r"(w.w)
-                                 : "memory");
-                    if (r >> 3 == u) asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(ns_peer(smem_u32(&D[r]), p)), "f"(d) : "memory");
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+                        asm volatile("st.shared::cluster.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(ns_peer(unit(h ? sl : sh, r, u), p)), "r"(w[h].x),
+                                     "r"(w[h].y), "r"(w[h].z), "r"(w[h].w) : "memory");
                 }
             }
             ns_fence_async();
@@ -879,59 +915,39 @@ __global__ void __launch_bounds__(kNsSmallThreads) k_ns_small(const __grid_const
             ns_cluster_arrive();
             ns_cluster_wait();
         }
-        product([&] {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                const unsigned long long d = ns_desc(ob + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024);
-                if (16 * k < mp) ns_mma<1>(ts, d, d, ns_idesc(128, mp, false), k > 0);
-            }
+        product([&] { squares(sh, sl, mp / 16); }, [&] {
+            if (a.C > 1)                                    // X's low half, where the parts were
+#pragma unroll 1
+                for (int c = x0; c < x1; c += 16) {
+                    float v[16];
+                    ns_ld16(tx + mine + c, v);
+                    uint4 h, l;
+                    ns_split8(v, 1.0f / kNsScale, h, l), ns_sts(unit(xl, row, c / 8), l);
+                    ns_split8(v + 8, 1.0f / kNsScale, h, l), ns_sts(unit(xl, row, c / 8 + 1), l);
+                }
         });
-        const float ca = a.c[3 * s], cb = a.c[3 * s + 1], cc = a.c[3 * s + 2] * (1.0f / kNsScale), d = D[row];
+        const float ca = a.c[3 * s] * kNsScale, cb = a.c[3 * s + 1], cc = a.c[3 * s + 2] * (1.0f / kNsScale);
 #pragma unroll 1
         for (int u = u0; u < u1; ++u) {
             float v[8];
             ns_ld8(ts + mine + 8 * u, v);
-            const bool on_diag = row >> 3 == u;
-            if (on_diag) {
-#pragma unroll
-                for (int q = 0; q < 8; ++q)
-                    if (row == 8 * u + q) E[row] = fmaf(cc, fmaf(d, d, v[q]), cb * d);
-            }
-            const uint4 o8 = ns_lds(unit(ob, row, u));
-            const float4 d0 = *(const float4*)&D[8 * u], d1 = *(const float4*)&D[8 * u + 4];
-            const float2 dj[4] = {{d0.x, d0.y}, {d0.z, d0.w}, {d1.x, d1.y}, {d1.z, d1.w}};
-            __half2 o4[4];
-            memcpy(o4, &o8, 16);
+            const uint4 h8 = ns_lds(unit(sh, row, u)), l8 = ns_lds(unit(sl, row, u));
+            __half2 h4[4], l4[4];
+            memcpy(h4, &h8, 16), memcpy(l4, &l8, 16);
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
-                const float2 o = __half22float2(o4[k]), x = make_float2(v[2 * k], v[2 * k + 1]);
-                const float2 f = f2_fma(f2_splat(cc), f2_fma(f2_add(f2_splat(d), dj[k]), o, x), f2_mul(f2_splat(cb), o));
+                const float2 o = f2_fma(__half22float2(l4[k]), f2_splat(1.0f / kNsLow), __half22float2(h4[k]));
+                const float2 f = f2_fma(f2_splat(cc), make_float2(v[2 * k], v[2 * k + 1]), f2_mul(f2_splat(cb), o));
                 v[2 * k] = f.x, v[2 * k + 1] = f.y;
             }
-            if (on_diag) {
+            if (row >> 3 == u) {
 #pragma unroll
                 for (int q = 0; q < 8; ++q)
-                    if (row == 8 * u + q) v[q] = 0;
+                    if (row == 8 * u + q) v[q] += ca;
             }
-            ns_sts(unit(pb, row, u), ns_half8(v, 1.0f));
+            store(sh, sl, u, v, 1.0f);
         }
-        __syncthreads();
-        const float e = fmaf(E[row], 1.0f / kNsScale, ca);
-#pragma unroll 1
-        for (int c = x0; c < x1; c += 16) {
-            float v[16];
-            ns_ld16(tx + mine + c, v);
-#pragma unroll
-            for (int q = 0; q < 16; ++q) v[q] *= e;
-            ns_st16(tx + mine + c, v);
-        }
-        ns_wait_st();
-        product([&] {
-            const unsigned idesc = ns_idesc(128, a.W, true);
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (16 * k < mp) ns_mma<1>(tx, ns_desc(pb + (k >> 2) * 16384 + (k & 3) * 32, 16, 1024), ns_desc(xh + k * 2048, 16384, 1024), idesc, 1);
-        });
+        product([&] { three(tx, sh, sl, xh, xl, mp / 16, true, ns_idesc(128, a.W, true)); }, [] {});
     }
     if (!ok) atomicAdd(a.giveups, 1u);
     const float unit_out = 1.0f / (kNsScale * a.sx);
@@ -1147,9 +1163,9 @@ static bool ns_small(NsSmall a, size_t batch, cudaStream_t st) {
     a.C = 1;
     while (a.C * kNsSmallWidth < a.N) a.C *= 2;
     a.W = ((a.N + a.C - 1) / a.C + 63) / 64 * 64;
-    const int smem = 1024 + a.W * 256 + 65536 + (a.C > 1 ? 65536 : 0);
+    const int smem = 1024 + a.W * 256 + ns_small_low(a.W, a.C) + 2 * ns_small_square(a.M);
     static std::atomic<uint64_t> done;
-    if (!allow_big_smem_once(k_ns_small<T>, 1024 + kNsSmallWidth * 256 + 131072, done)) return false;
+    if (!allow_big_smem_once(k_ns_small<T>, 1024 + kNsSmallWidth * 256 + 65536 + 2 * 32768, done)) return false;
     if (a.C > 8 && cudaFuncSetAttribute(k_ns_small<T>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) != cudaSuccess) return false;
     cudaLaunchConfig_t cfg = {};
     cudaLaunchAttribute attr[1];
