@@ -8,12 +8,15 @@
 // On chip (k_ns_small: a side of at most 128, the other up to 4096) all three products take both halves of both operands, hi lo +
 // lo hi + hi hi; B includes a I.  The result is then within 0.05 % of the 64-bit one for every spectrum and for steep
 // coefficients, 0.01 % mostly.
-// In the tiled kernels hi alone is the operand and the carried term a X uses both.  A and B are nearly diagonal once the singular
+// In the tiled kernels hi is the operand and the carried term a X uses both.  A and B are nearly diagonal once the singular
 // values are near 1, so their diagonals are kept apart, in binary32, and only the rest is rounded to binary16:
 //     A = D + O,  B = E + P:  P = b O + c (O O + (D_i + D_j) O) off the diagonal, E = b D + c (O O + D D) on it,
 //     X <- (a + E_i) X + P X,
-// which takes the diagonal's products out of the rounded operands.  The result is then within 0.04 - 0.1 % of the 64-bit one for
-// noise (diagonals inside A and B: 0.15 - 0.2 %; hi alone for the carried term: 2 - 7 % at low rank).
+// which takes the diagonal's products out of the rounded operands.  X's low half is multiplied with P too in the steps whose
+// rounding would still grow (kNsLowFrom), and for few rows O and P have low halves (kNsFine).  The result is then within 0.05 -
+// 0.1 % of the 64-bit one for noise, 0.04 % for one strong direction over weak ones, 0.02 - 0.4 % for a constant level over small
+// noise, whose equal entries are all rounded the same way (diagonals inside A and B: 0.15 - 0.2 % for noise; X's hi alone: 0.3 % at 129
+// rows for one strong direction, and 2 - 7 % at low rank if the carried term has no more).
 // Scaling by powers of two keeps everything in binary16's normal range: X times sx ~ sqrt(N), A and B times 256, lo times 2^11.
 //
 // Products with 128 x 128 tiles, one CTA each (k_ns_tile); the sum over K may be split over a cluster of 2 or 4 CTAs, which add
@@ -49,15 +52,24 @@ struct NsArgs {
     const float* diag;      // POLY: D of A, APPLY and LAST: E of B (times kNsScale)
     float* diag_out;        // GRAM: D, POLY: E
     const __half* hi;       // POLY: O, APPLY and LAST: X hi
-    const __half* lo;       // X lo
+    const __half* lo;       // X lo; POLY: O lo or NULL
     __half* out;            // O, P or the new X hi
-    __half* out_lo;         // new X lo
+    __half* out_lo;         // new X lo; O lo, P lo or NULL
+    int low;                // products before that of the high halves: 1 left hi with right lo, 2 left lo with right hi
     __nv_bfloat16* last;    // LAST: the result
     long long last_row, last_col, last_mat;     // its strides
     bool last_vec;          // its rows start on 16-byte boundaries
     int tiles_m, tiles_n, tiles;                // k_ns_pair: 256 x 256 tiles of a matrix, and all of them
     unsigned* giveups;
 };
+
+// the operands' high and low halves (the latter where they are asked for)
+struct NsMaps {
+    CUtensorMap left, right, left_low, right_low;
+};
+// Which halves are multiplied: 1 left's high with right's low, 2 left's low with right's high, 0 the high halves, always and last
+__device__ __forceinline__ int ns_first(int low) { return low & 1 ? 1 : low; }
+__device__ __forceinline__ int ns_next(int which, int low) { return which == 1 ? low & 2 : 0; }
 
 __device__ __forceinline__ bool ns_wait(unsigned bar, unsigned parity) {
     unsigned done = 0;
@@ -114,13 +126,17 @@ __device__ __forceinline__ void ns_mma_shift(unsigned tmem, unsigned long long a
         asm volatile("{\n\t.reg .pred p, e;\n\telect.sync _|e, 0xffffffff;\n\tsetp.eq.s32 p, 0, 0;\n\t"
                      "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p, 11;\n\t}" ::"r"(tmem), "l"(a), "l"(b), "r"(idesc) : "memory");
 }
-// one stage: K = 64 in four products.  left: 128 rows of 128 bytes; right: the same, or (N_MAJOR) 64 rows of K for every 64 columns
+// one stage: K = 64 in four products.  left: 128 rows of 128 bytes; right: the same, or (N_MAJOR) 64 rows of K for every 64 columns.
+// shift: the first stage behind those with low halves
 template <int CG, bool N_MAJOR>
-__device__ __forceinline__ void ns_mma_stage(unsigned tmem, unsigned left, unsigned right, unsigned idesc, bool add) {
+__device__ __forceinline__ void ns_mma_stage(unsigned tmem, unsigned left, unsigned right, unsigned idesc, bool add, bool shift) {
 #pragma unroll
-    for (int q = 0; q < kNsK / 16; ++q)
-        ns_mma<CG>(tmem, ns_desc(left + 32 * q, 16, 1024), N_MAJOR ? ns_desc(right + 2048 * q, 8192, 1024) : ns_desc(right + 32 * q, 16, 1024), idesc,
-                   add || q);
+    for (int q = 0; q < kNsK / 16; ++q) {
+        const unsigned long long a = ns_desc(left + 32 * q, 16, 1024);
+        const unsigned long long b = N_MAJOR ? ns_desc(right + 2048 * q, 8192, 1024) : ns_desc(right + 32 * q, 16, 1024);
+        if (q == 0 && shift) ns_mma_shift<CG>(tmem, a, b, idesc);
+        else ns_mma<CG>(tmem, a, b, idesc, add || q);
+    }
 }
 template <int CG>
 __device__ __forceinline__ void ns_commit(unsigned bar) {       // a whole warp; CG = 2: arrives at the same place of both CTAs
@@ -200,7 +216,7 @@ __device__ __forceinline__ void ns_fetch(const NsArgs& a, int z, int i0, int j, 
         for (int k = 0; k < 4; ++k)
             if (i0 + r + 8 * k < a.M) {
                 ns_async16(ns_unit(buf, r + 8 * k, u), a.hi + at + (size_t)8 * k * a.ld);
-                if (MODE != NS_POLY) ns_async16(ns_unit(buf + kNsWarpBuf, r + 8 * k, u), a.lo + at + (size_t)8 * k * a.ld);
+                if (MODE != NS_POLY || a.lo) ns_async16(ns_unit(buf + kNsWarpBuf, r + 8 * k, u), a.lo + at + (size_t)8 * k * a.ld);
             }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -210,6 +226,16 @@ __device__ __forceinline__ unsigned ns_bits(__half2 h) {
     unsigned u;
     memcpy(&u, &h, 4);
     return u;
+}
+
+// a lane's row of 32 values, two to a word, into the transposed image [column][32 rows]
+__device__ __forceinline__ void ns_mirror(unsigned buf, int lane, const unsigned (&row)[16]) {
+    const unsigned to = buf + kNsWarpBuf + lane * 2;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) {
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 128 * k), "h"((unsigned short)(row[k] & 0xffff)) : "memory");
+        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 128 * k + 64), "h"((unsigned short)(row[k] >> 16)) : "memory");
+    }
 }
 
 // get(c, v): the sums of columns c .. c + 31 of this lane's row; cols: a multiple of 32.  ns_fetch has been called for the first 32.
@@ -237,29 +263,32 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 if (i == j + q) on_diag = MODE == NS_GRAM ? a.alpha * v[q] : fmaf(a.alpha, fmaf(d, d, v[q]), a.b * d);
             if (row) a.diag_out[dd + i] = on_diag;
         }
+        unsigned hi[16], low[16];                           // A and B: the row, for the mirror image and the low halves behind the loop
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const unsigned at = ns_unit(buf, lane, q);
             uint4 u;
             __half2 h[4], l[4];
             if (MODE != NS_GRAM) u = ns_lds(at), memcpy(h, &u, 16);
-            if (MODE >= NS_APPLY) u = ns_lds(at + kNsWarpBuf), memcpy(l, &u, 16);
+            if (MODE >= NS_APPLY || (MODE == NS_POLY && a.lo)) u = ns_lds(at + kNsWarpBuf), memcpy(l, &u, 16);
             float4 dj[2];
             if (MODE == NS_POLY) {                          // the same for all lanes; up to the pitch, which is a multiple of 64
                 dj[0] = *(const float4*)(a.diag + dd + j + 8 * q);
                 dj[1] = *(const float4*)(a.diag + dd + j + 8 * q + 4);
             }
-            unsigned hb[4], lb[4];
+            unsigned hb[4], lb[4] = {};
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 float2 x = make_float2(v[8 * q + 2 * k], v[8 * q + 2 * k + 1]);
                 if (MODE == NS_GRAM) {
                     x = f2_mul(x, alpha);
                 } else if (MODE == NS_POLY) {
-                    const float2 o = __half22float2(h[k]), s = k & 1 ? make_float2(dj[k / 2].z, dj[k / 2].w) : make_float2(dj[k / 2].x, dj[k / 2].y);
+                    float2 o = __half22float2(h[k]);
+                    if (a.lo) o = f2_fma(__half22float2(l[k]), f2_splat(1.0f / kNsLow), o);
+                    const float2 s = k & 1 ? make_float2(dj[k / 2].z, dj[k / 2].w) : make_float2(dj[k / 2].x, dj[k / 2].y);
                     x = f2_fma(alpha, f2_fma(f2_add(d2, s), o, x), f2_mul(b, o));
                 } else {
-                    x = f2_fma(e, f2_fma(__half22float2(l[k]), f2_splat(1.0f / 2048), __half22float2(h[k])), f2_mul(alpha, x));
+                    x = f2_fma(e, f2_fma(__half22float2(l[k]), f2_splat(1.0f / kNsLow), __half22float2(h[k])), f2_mul(alpha, x));
                 }
                 if (here) {
                     if (i == j + 8 * q + 2 * k) x.x = 0;
@@ -272,14 +301,11 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 } else {
                     const __half2 y = __floats2half2_rn(x.x, x.y);
                     hb[k] = ns_bits(y);
-                    if (MODE == NS_APPLY) {
-                        const float2 r = f2_mul(f2_fma(__half22float2(y), f2_splat(-1.0f), x), f2_splat(2048.0f));
+                    if (MODE == NS_APPLY || a.out_lo) {
+                        const float2 r = f2_mul(f2_fma(__half22float2(y), f2_splat(-1.0f), x), f2_splat(kNsLow));
                         lb[k] = ns_bits(__floats2half2_rn(r.x, r.y));
-                    } else if (mirror) {                    // transposed: [column][32 rows]
-                        const unsigned to = buf + kNsWarpBuf + (8 * q + 2 * k) * 64 + lane * 2;
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((unsigned short)(hb[k] & 0xffff)) : "memory");
-                        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 64), "h"((unsigned short)(hb[k] >> 16)) : "memory");
                     }
+                    if (MODE != NS_APPLY) hi[4 * q + k] = hb[k], low[4 * q + k] = lb[k];
                 }
             }
             ns_sts(at, make_uint4(hb[0], hb[1], hb[2], hb[3]));
@@ -292,6 +318,10 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 if (j + q < a.N) to[q * a.last_col] = __float2bfloat16_rn(v[q]);
         }
         __syncwarp();
+        if (MODE <= NS_POLY && mirror) {
+            ns_mirror(buf, lane, hi);
+            __syncwarp();
+        }
         const int r = lane >> 2, u = lane & 3;
         if (MODE == NS_LAST) {
             if (a.last_col == 1) {
@@ -312,19 +342,29 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 }
             }
         } else {
-            const size_t at = (size_t)z * a.mat + (size_t)(i0 + r) * a.ld + j + 8 * u;
+            auto write = [&](__half* to, unsigned from) {
+                to += (size_t)z * a.mat + (size_t)(i0 + r) * a.ld + j + 8 * u;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (i0 + r + 8 * k < a.M) {
-                    *(uint4*)(a.out + at + (size_t)8 * k * a.ld) = ns_lds(ns_unit(buf, r + 8 * k, u));
-                    if (MODE == NS_APPLY) *(uint4*)(a.out_lo + at + (size_t)8 * k * a.ld) = ns_lds(ns_unit(buf + kNsWarpBuf, r + 8 * k, u));
-                }
-            if (MODE != NS_APPLY && mirror && i0 < a.M) {
-                // 8 columns of 64 bytes at a time; elements behind row M - 1 fall into the pitch
-                __half* to = a.out + (size_t)z * a.mat + (size_t)(j + r) * a.ld + i0 + 8 * u;
+                for (int k = 0; k < 4; ++k)
+                    if (i0 + r + 8 * k < a.M) *(uint4*)(to + (size_t)8 * k * a.ld) = ns_lds(ns_unit(from, r + 8 * k, u));
+            };
+            auto write_mirror = [&](__half* to) {           // 8 columns of 64 bytes at a time; elements behind row M - 1 fall into the pitch
+                to += (size_t)z * a.mat + (size_t)(j + r) * a.ld + i0 + 8 * u;
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     if (j + r + 8 * k < a.N) *(uint4*)(to + (size_t)8 * k * a.ld) = ns_lds(buf + kNsWarpBuf + (r + 8 * k) * 64 + u * 16);
+            };
+            write(a.out, buf);
+            if (MODE == NS_APPLY) write(a.out_lo, buf + kNsWarpBuf);
+            if (MODE != NS_APPLY && mirror && i0 < a.M) write_mirror(a.out);
+            if (MODE != NS_APPLY && a.out_lo) {             // the low halves the same way
+                __syncwarp();
+#pragma unroll
+                for (int q = 0; q < 4; ++q) ns_sts(ns_unit(buf, lane, q), make_uint4(low[4 * q], low[4 * q + 1], low[4 * q + 2], low[4 * q + 3]));
+                if (mirror) ns_mirror(buf, lane, low);
+                __syncwarp();
+                write(a.out_lo, buf);
+                if (mirror && i0 < a.M) write_mirror(a.out_lo);
             }
         }
         __syncwarp();
@@ -342,8 +382,7 @@ __device__ __forceinline__ void ns_landed(unsigned bar, unsigned n) {
 // is filling the stages from L2, K / 64 blocks of products, the exchange of a split and one epilogue.  512 x 512: 107 us for 15
 // of these and the two launches before them, 6 to 7 us each.
 template <int MODE>
-__global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant__ CUtensorMap left,
-                                                           const __grid_constant__ CUtensorMap right,
+__global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant__ NsMaps maps,
                                                            const __grid_constant__ NsArgs a, int split) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     extern __shared__ unsigned char raw[];
@@ -357,8 +396,8 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
     auto empty = [&](int s) { return bar + 8 * (kNsMaxStages + s); };
     const unsigned done = bar + 8 * 2 * kNsMaxStages, left_off = done + 8;
     if (threadIdx.x == 32 * kNsEpilogueWarps) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.left) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.right) : "memory");
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * kNsMaxStages + 2; ++s) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + 8 * s) : "memory");
@@ -382,31 +421,40 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
     pdl_wait();
     if (warp == kNsEpilogueWarps) {
         if (lane == 0) {
-            int k = 0;
-            for (int s = 0, ph = 1; k < nk; ++k) {
-                if (!(ok = ns_wait(empty(s), ph))) break;
-                const unsigned dst = base + s * kNsStageBytes;
-                const int x = (k0 + k) * kNsK;
-                ns_expect(full(s), kNsStageBytes);
-                ns_load<1>(dst, &left, x, i0, z, full(s));
-                if (kSym) {
-                    ns_load<1>(dst + kNsHalf, &right, x, j0, z, full(s));
-                } else {
-                    ns_load<1>(dst + kNsHalf, &right, j0, x, z, full(s));
-                    ns_load<1>(dst + kNsHalf + 8192, &right, j0 + 64, x, z, full(s));
+            unsigned loads = 0;
+            for (int s = 0, ph = 1, which = ns_first(a.low); ok; which = ns_next(which, a.low)) {
+                const CUtensorMap* const l = which == 2 ? &maps.left_low : &maps.left;
+                const CUtensorMap* const r = which == 1 ? &maps.right_low : &maps.right;
+                for (int k = 0; k < nk; ++k) {
+                    if (!(ok = ns_wait(empty(s), ph))) break;
+                    const unsigned dst = base + s * kNsStageBytes;
+                    const int x = (k0 + k) * kNsK;
+                    ns_expect(full(s), kNsStageBytes);
+                    ns_load<1>(dst, l, x, i0, z, full(s));
+                    if (kSym) {
+                        ns_load<1>(dst + kNsHalf, r, x, j0, z, full(s));
+                    } else {
+                        ns_load<1>(dst + kNsHalf, r, j0, x, z, full(s));
+                        ns_load<1>(dst + kNsHalf + 8192, r, j0 + 64, x, z, full(s));
+                    }
+                    ++loads;
+                    if (++s == kNsMaxStages) s = 0, ph ^= 1;
                 }
-                if (++s == kNsMaxStages) s = 0, ph ^= 1;
+                if (!which) break;
             }
-            ns_landed(bar, k);
+            ns_landed(bar, loads);
         }
     } else if (warp == kNsEpilogueWarps + 1) {
-        for (int k = 0, s = 0, ph = 0; k < nk; ++k) {
-            if (!(ok = __all_sync(~0u, ns_wait(full(s), ph)))) break;
-            ns_fence_after();
-            const unsigned l = base + s * kNsStageBytes;
-            ns_mma_stage<1, !kSym>(tmem, l, l + kNsHalf, ns_idesc(128, 128, !kSym), k > 0);
-            ns_commit<1>(empty(s));
-            if (++s == kNsMaxStages) s = 0, ph ^= 1;
+        for (int s = 0, ph = 0, which = ns_first(a.low); ok; which = ns_next(which, a.low)) {
+            for (int k = 0; k < nk; ++k) {
+                if (!(ok = __all_sync(~0u, ns_wait(full(s), ph)))) break;
+                ns_fence_after();
+                const unsigned l = base + s * kNsStageBytes;
+                ns_mma_stage<1, !kSym>(tmem, l, l + kNsHalf, ns_idesc(128, 128, !kSym), k > 0 || which != ns_first(a.low), a.low && !which && !k);
+                ns_commit<1>(empty(s));
+                if (++s == kNsMaxStages) s = 0, ph ^= 1;
+            }
+            if (!which) break;
         }
         ns_commit<1>(ok ? done : left_off);
         if (!ok) ns_wait(left_off, 0);                      // its products too
@@ -497,8 +545,7 @@ __device__ __forceinline__ void ns_tile_at(const NsArgs& a, int t, int* z, int* 
 // products; a tile's epilogue runs beside the next tile's products.  4096 x 4096: 59 us for A, 62 for B (half the tiles each), 112
 // for X, the tensor pipe 61 - 65 % busy: 136 tiles of A are 1.8 turns of 74 pairs.
 template <int MODE>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_pair(const __grid_constant__ CUtensorMap left,
-                                                                                     const __grid_constant__ CUtensorMap right,
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_pair(const __grid_constant__ NsMaps maps,
                                                                                      const __grid_constant__ NsArgs a) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     extern __shared__ unsigned char raw[];
@@ -514,8 +561,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
     auto taken = [&](int t) { return bar + 8 * (2 * kNsMaxStages + 2 + t); };   // CTA 0's: both CTAs' epilogue warps have read them
     const unsigned left_off = bar + 8 * (2 * kNsMaxStages + 4);                 // each CTA's: products issued before a wait ran out
     if (threadIdx.x == 32 * kNsEpilogueWarps) {
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&left) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&right) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.left) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&maps.right) : "memory");
     }
     if (threadIdx.x == 0) {
         for (int s = 0; s < 2 * kNsMaxStages + 5; ++s)
@@ -545,19 +592,24 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
                 int ti, tj, z;
                 ns_tile_at<kSym>(a, n, &z, &ti, &tj);
                 const int i0 = ti * 256 + 128 * rank, j0 = tj * 256 + 128 * rank;
-                for (int k = 0; k < nk; ++k) {
-                    if (!(ok = ns_wait(empty(s), ph))) break;
-                    const unsigned dst = base + s * kNsStageBytes, at = ns_peer(full(s), 0);
-                    if (rank == 0) ns_expect(full(s), 2 * kNsStageBytes);
-                    ns_load<2>(dst, &left, k * kNsK, i0, z, at);
-                    if (kSym) {
-                        ns_load<2>(dst + kNsHalf, &right, k * kNsK, j0, z, at);
-                    } else {
-                        ns_load<2>(dst + kNsHalf, &right, j0, k * kNsK, z, at);
-                        ns_load<2>(dst + kNsHalf + 8192, &right, j0 + 64, k * kNsK, z, at);
+                for (int which = ns_first(a.low); ok; which = ns_next(which, a.low)) {
+                    const CUtensorMap* const l = which == 2 ? &maps.left_low : &maps.left;
+                    const CUtensorMap* const r = which == 1 ? &maps.right_low : &maps.right;
+                    for (int k = 0; k < nk; ++k) {
+                        if (!(ok = ns_wait(empty(s), ph))) break;
+                        const unsigned dst = base + s * kNsStageBytes, at = ns_peer(full(s), 0);
+                        if (rank == 0) ns_expect(full(s), 2 * kNsStageBytes);
+                        ns_load<2>(dst, l, k * kNsK, i0, z, at);
+                        if (kSym) {
+                            ns_load<2>(dst + kNsHalf, r, k * kNsK, j0, z, at);
+                        } else {
+                            ns_load<2>(dst + kNsHalf, r, j0, k * kNsK, z, at);
+                            ns_load<2>(dst + kNsHalf + 8192, r, j0 + 64, k * kNsK, z, at);
+                        }
+                        ++loads;
+                        if (++s == kNsMaxStages) s = 0, ph ^= 1;
                     }
-                    ++loads;
-                    if (++s == kNsMaxStages) s = 0, ph ^= 1;
+                    if (!which) break;
                 }
             }
             if (rank == 0) ns_landed(bar, loads);           // both CTAs' copies; the other CTA waits for this one before it leaves
@@ -568,13 +620,17 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
             for (int s = 0, ph = 0, n = pair; n < a.tiles && ok; n += pairs) {
                 if (!(ok = __all_sync(~0u, ns_wait(taken(t), tph)))) break;
                 ns_fence_after();
-                for (int k = 0; k < nk; ++k) {
-                    if (!(ok = __all_sync(~0u, ns_wait(full(s), ph)))) break;
-                    ns_fence_after();
-                    const unsigned l = base + s * kNsStageBytes;
-                    ns_mma_stage<2, !kSym>(tmem + 256 * t, l, l + kNsHalf, ns_idesc(256, 256, !kSym), k > 0);
-                    ns_commit<2>(empty(s));
-                    if (++s == kNsMaxStages) s = 0, ph ^= 1;
+                for (int which = ns_first(a.low); ok; which = ns_next(which, a.low)) {
+                    for (int k = 0; k < nk; ++k) {
+                        if (!(ok = __all_sync(~0u, ns_wait(full(s), ph)))) break;
+                        ns_fence_after();
+                        const unsigned l = base + s * kNsStageBytes;
+                        ns_mma_stage<2, !kSym>(tmem + 256 * t, l, l + kNsHalf, ns_idesc(256, 256, !kSym), k > 0 || which != ns_first(a.low),
+                                               a.low && !which && !k);
+                        ns_commit<2>(empty(s));
+                        if (++s == kNsMaxStages) s = 0, ph ^= 1;
+                    }
+                    if (!which) break;
                 }
                 if (ok) ns_commit<2>(sums(t));
                 if (++t == 2) t = 0, tph ^= 1;
@@ -1069,9 +1125,14 @@ __global__ void __launch_bounds__(256) k_ns_prepare(const T* __restrict__ g, int
     }
 }
 
+// Tiled kernels: up to this M the square matrices have low halves too.  That takes the roundings of P away, which fall on few rows
+// there (16 x 8192, one direction over 1e-5: 0.12 -> 0.004 %, 3 x 9000, a level over noise 0.10 -> 0.04 %), for 104 -> 119 us at
+// 16 x 8192; 200 x 300 would go from 117 to 143 us and from 0.08 to 0.06 %.
+constexpr int kNsFine = 128;
 struct NsLayout {
     int M, N, ldm, ldn, parts;
-    size_t xmat, amat, part_off, x0, x1, xl, a_off, b_off, da, db, bytes;
+    size_t xmat, amat, part_off, x0, x1, l0, l1, a_off, b_off, al, bl, da, db, bytes;
+    bool fine;              // A and B have low halves too
 };
 static NsLayout ns_layout(size_t batch, size_t rows, size_t cols) {
     NsLayout L;
@@ -1087,10 +1148,14 @@ static NsLayout ns_layout(size_t batch, size_t rows, size_t cols) {
     L.part_off = 0;
     L.x0 = up(batch * L.parts * sizeof(double));
     L.x1 = L.x0 + up(batch * L.xmat * 2);
-    L.xl = L.x1 + up(batch * L.xmat * 2);
-    L.a_off = L.xl + up(batch * L.xmat * 2);
+    L.l0 = L.x1 + up(batch * L.xmat * 2);
+    L.l1 = L.l0 + up(batch * L.xmat * 2);
+    L.a_off = L.l1 + up(batch * L.xmat * 2);
     L.b_off = L.a_off + up(batch * L.amat * 2);
-    L.da = L.b_off + up(batch * L.amat * 2);
+    L.fine = L.M <= kNsFine;
+    L.al = L.b_off + up(batch * L.amat * 2);
+    L.bl = L.al + (L.fine ? up(batch * L.amat * 2) : 0);
+    L.da = L.bl + (L.fine ? up(batch * L.amat * 2) : 0);
     L.db = L.da + up(batch * (size_t)L.ldm * 4);
     L.bytes = L.db + up(batch * (size_t)L.ldm * 4);
     return L;
@@ -1110,7 +1175,7 @@ static bool ns_map(CUtensorMap* out, void* base, int inner, int rows, size_t bat
 // 1024 x 1024 210 us against 142; one part alone 512 x 2048 154 us against 132 (the last two with slower epilogues).
 constexpr int kNsSplitMax = 128;
 template <int MODE>
-static bool ns_product(const CUtensorMap& left, const CUtensorMap& right, NsArgs a, int batch, cudaStream_t st) {
+static bool ns_product(const NsMaps& maps, NsArgs a, int batch, cudaStream_t st) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     auto count = [&](int t) {
         const long long m = (a.M + t - 1) / t, n = (a.N + t - 1) / t;
@@ -1130,7 +1195,7 @@ static bool ns_product(const CUtensorMap& left, const CUtensorMap& right, NsArgs
         a.tiles_m = (a.M + 255) / 256, a.tiles_n = (a.N + 255) / 256, a.tiles = (int)big;
         cfg.gridDim = dim3((unsigned)(2 * (big < kSMs / 2 ? big : kSMs / 2)));
         if (!allow_big_smem_once(k_ns_pair<MODE>, smem, done[0])) return false;
-        e = cudaLaunchKernelEx(&cfg, k_ns_pair<MODE>, left, right, a);
+        e = cudaLaunchKernelEx(&cfg, k_ns_pair<MODE>, maps, a);
     } else {
         int split = 1;
         while (split < 4 && small * split * 2 <= kNsSplitMax && a.K / kNsK >= split * 16) split *= 2;
@@ -1139,7 +1204,7 @@ static bool ns_product(const CUtensorMap& left, const CUtensorMap& right, NsArgs
         attr[1].val.clusterDim = {(unsigned)split, 1, 1};
         cfg.numAttrs = 2;
         if (!allow_big_smem_once(k_ns_tile<MODE>, smem, done[1])) return false;
-        e = cudaLaunchKernelEx(&cfg, k_ns_tile<MODE>, left, right, a, split);
+        e = cudaLaunchKernelEx(&cfg, k_ns_tile<MODE>, maps, a, split);
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess;
@@ -1153,7 +1218,7 @@ static void ns_start(const void* g, size_t batch, size_t rows, size_t cols, size
     TRV_LAUNCH(k_ns_norm<T>, dim3(L.parts, (unsigned)batch), 256, 0, st, (const T*)g, (int)rows, (int)cols, (long long)row, (long long)mat, vec, part);
     launch_pdl(k_ns_prepare<T>, dim3((unsigned)(cols + 63) / 64, (unsigned)(rows + 63) / 64, (unsigned)batch), dim3(256), 0, st, (const T*)g,
                (int)rows, (int)cols, (long long)row, (long long)mat, (const double*)part, L.parts, eps, sx, (int)(rows > cols), (__half*)(ws + L.x0),
-               (__half*)(ws + L.xl), L.ldn, L.xmat);
+               (__half*)(ws + L.l0), L.ldn, L.xmat);
 }
 
 // Matrices that k_ns_small takes: M <= 128 and columns for at most a cluster of 16
@@ -1181,6 +1246,12 @@ static bool ns_small(NsSmall a, size_t batch, cudaStream_t st) {
 constexpr size_t kNsMaxSide = (size_t)1 << 20, kNsMaxBatch = 65535;
 constexpr float kNsDefault[3] = {3.4445f, -4.7750f, 2.0315f};
 constexpr int kNsMaxSteps = 64;
+// Tiled kernels: in which steps P is multiplied with X's low half too.  What it rounds off a strong direction falls, through P's
+// part outside the diagonal, on all the others, 2^-12 / M times about 10 of the strong one, and grows with them in later steps:
+// with X's high half alone one strong direction over weak ones ended 2.9 % off at 16 rows, 0.3 % at 129, 0.08 % at 512, 0.04 % at
+// 2048.  A step's share is kept below 1e-4, where it drowns in the other roundings: low half if 24 times the growth still to
+// come exceeds M.  Default coefficients: three steps of five at M = 200, the first at 1024, none from 3379 on.
+constexpr double kNsLowFrom = 24;
 
 }  // namespace trv
 
@@ -1224,7 +1295,8 @@ extern "C" trv_status_t trv_orthogonalize(const void* g, void* out, size_t batch
     const cudaStream_t st = (cudaStream_t)cuda_stream;
     unsigned char* ws = (unsigned char*)workspace;
     __half* X[2] = {(__half*)(ws + L.x0), (__half*)(ws + L.x1)};
-    __half *xl = (__half*)(ws + L.xl), *A = (__half*)(ws + L.a_off), *B = (__half*)(ws + L.b_off);
+    __half* lo[2] = {(__half*)(ws + L.l0), (__half*)(ws + L.l1)};
+    __half *A = (__half*)(ws + L.a_off), *B = (__half*)(ws + L.b_off);
     float *DA = (float*)(ws + L.da), *DB = (float*)(ws + L.db);
     int e = 0;                                              // sx = 2^e, nearest to sqrt(N)
     while (((size_t)2 << (2 * e)) <= (size_t)L.N) ++e;
@@ -1240,34 +1312,43 @@ extern "C" trv_status_t trv_orthogonalize(const void* g, void* out, size_t batch
         g_last_kernel = "orthogonalize_small";
         return ok && cudaGetLastError() == cudaSuccess ? TRV_OK : TRV_ERR_CUDA;
     }
-    CUtensorMap xk[2], xn[2], ak, bk;
+    CUtensorMap xk[2], xn[2], ln[2], ak, bk, akl = {}, bkl = {};
+    __half *al = L.fine ? (__half*)(ws + L.al) : nullptr, *bl = L.fine ? (__half*)(ws + L.bl) : nullptr;
     for (int p = 0; p < 2 && ok; ++p)
-        ok = ns_map(&xk[p], X[p], L.N, L.M, batch, L.ldn, L.xmat, kNsTile) && ns_map(&xn[p], X[p], L.N, L.M, batch, L.ldn, L.xmat, kNsK);
+        ok = ns_map(&xk[p], X[p], L.N, L.M, batch, L.ldn, L.xmat, kNsTile) && ns_map(&xn[p], X[p], L.N, L.M, batch, L.ldn, L.xmat, kNsK) &&
+             ns_map(&ln[p], lo[p], L.N, L.M, batch, L.ldn, L.xmat, kNsK);
     ok = ok && ns_map(&ak, A, L.M, L.M, batch, L.ldm, L.amat, kNsTile) && ns_map(&bk, B, L.M, L.M, batch, L.ldm, L.amat, kNsTile);
+    if (L.fine) ok = ok && ns_map(&akl, al, L.M, L.M, batch, L.ldm, L.amat, kNsTile) && ns_map(&bkl, bl, L.M, L.M, batch, L.ldm, L.amat, kNsTile);
     if (!ok) return TRV_ERR_CUDA;
     if (dtype == TRV_FLOAT32) ns_start<float>(g, batch, rows, cols, g_stride, g_batch_stride, eps, sx, L, ws, st);
     else if (dtype == TRV_BFLOAT16) ns_start<__nv_bfloat16>(g, batch, rows, cols, g_stride, g_batch_stride, eps, sx, L, ws, st);
     else ns_start<__half>(g, batch, rows, cols, g_stride, g_batch_stride, eps, sx, L, ws, st);
     const bool tall = rows > cols;
     for (int s = 0; s < steps && ok; ++s) {
-        const float* c = coefficients ? coefficients + 3 * s : kNsDefault;
+        auto step = [&](int t) { return coefficients ? coefficients + 3 * t : kNsDefault; };
+        const float* c = step(s);
         const int p = s & 1;
+        double grows = 1;                                   // by this factor in the later steps, if weak enough
+        for (int t = s + 1; t < steps; ++t) grows *= fabs((double)step(t)[0]);
         NsArgs k = {};
         k.Md = L.ldm, k.a = c[0], k.b = c[1], k.giveups = giveups;
         NsArgs gram = k, poly = k, apply = k;
         gram.M = gram.N = poly.M = poly.N = poly.K = apply.M = apply.K = L.M;
         gram.K = apply.N = L.N;
         gram.ld = poly.ld = L.ldm, gram.mat = poly.mat = L.amat, apply.ld = L.ldn, apply.mat = L.xmat;
-        gram.alpha = kNsScale / (sx * sx), gram.out = A, gram.diag_out = DA;
+        gram.alpha = kNsScale / (sx * sx), gram.out = A, gram.out_lo = al, gram.diag_out = DA;
         poly.alpha = c[2] / kNsScale, poly.hi = A, poly.diag = DA, poly.out = B, poly.diag_out = DB;
+        poly.lo = al, poly.out_lo = bl, poly.low = L.fine ? 3 : 0;
         const bool last = s + 1 == steps;
-        apply.unit = last ? 1.0f / sx : 1.0f, apply.alpha = apply.unit / kNsScale, apply.hi = X[p], apply.lo = xl, apply.diag = DB;
-        apply.out = X[1 - p], apply.out_lo = xl, apply.last = (__nv_bfloat16*)out;
+        apply.unit = last ? 1.0f / sx : 1.0f, apply.alpha = apply.unit / kNsScale, apply.hi = X[p], apply.lo = lo[p], apply.diag = DB;
+        apply.low = (kNsLowFrom * grows > L.M ? 1 : 0) | (L.fine ? 2 : 0);
+        apply.out = X[1 - p], apply.out_lo = lo[1 - p], apply.last = (__nv_bfloat16*)out;
         apply.last_row = (long long)(tall ? 1 : out_stride), apply.last_col = (long long)(tall ? out_stride : 1);
         apply.last_mat = (long long)out_batch_stride;
         apply.last_vec = !misaligned(out, 16) && out_stride % 8 == 0 && (batch == 1 || out_batch_stride % 8 == 0);
-        ok = ns_product<NS_GRAM>(xk[p], xk[p], gram, (int)batch, st) && ns_product<NS_POLY>(ak, ak, poly, (int)batch, st) &&
-             (last ? ns_product<NS_LAST>(bk, xn[p], apply, (int)batch, st) : ns_product<NS_APPLY>(bk, xn[p], apply, (int)batch, st));
+        const NsMaps xx = {xk[p], xk[p], xk[p], xk[p]}, aa = {ak, ak, akl, akl}, bx = {bk, xn[p], bkl, ln[p]};
+        ok = ns_product<NS_GRAM>(xx, gram, (int)batch, st) && ns_product<NS_POLY>(aa, poly, (int)batch, st) &&
+             (last ? ns_product<NS_LAST>(bx, apply, (int)batch, st) : ns_product<NS_APPLY>(bx, apply, (int)batch, st));
     }
     g_last_kernel = "orthogonalize";
     return ok && cudaGetLastError() == cudaSuccess ? TRV_OK : TRV_ERR_CUDA;

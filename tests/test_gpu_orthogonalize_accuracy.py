@@ -66,3 +66,37 @@ def test_a_level_over_small_noise_on_chip(rows, cols):
 def test_steep_steps_on_chip(rows, cols, seed):
     _check(_noise(rows, cols, seed=seed), 1e-3, STEEP)
     _check(_strong(rows, cols, 1e-3, seed), 1e-3, STEEP)
+
+
+TILED = [(129, 129), (150, 200), (200, 300), (300, 1000), (1000, 300), (512, 512), (1024, 600), (700, 1100), (2300, 2100)]
+THIN = [(3, 9000), (16, 8192), (40, 5000), (9001, 100)]                    # a side of at most 128, the other too long to stay on chip
+
+
+@pytest.mark.parametrize("weak", [1e-2, 1e-3, 1e-4, 1e-5])
+@pytest.mark.parametrize("rows,cols", TILED + THIN)
+def test_one_strong_direction_tiled(rows, cols, weak):
+    _check(_strong(rows, cols, weak), 1e-3)
+
+
+@pytest.mark.parametrize("rows,cols", TILED + THIN)
+def test_a_level_over_small_noise_tiled(rows, cols):
+    """Roundings of A and B beside the diagonal, which the strong direction fills evenly."""
+    _check(_noise(rows, cols, 1.0, 1e-3), 2.5e-3)
+    _check(_noise(rows, cols, 1.0, 1e-4, 1), 2.5e-3)
+
+
+@pytest.mark.parametrize("rows,cols", TILED)
+def test_steep_steps_tiled(rows, cols):
+    """Every rounding to binary16 counts up to 40 times."""
+    _check(_noise(rows, cols), 7.5e-3, STEEP)
+    _check(_strong(rows, cols, 1e-3), 7.5e-3, STEEP)
+
+
+def test_one_strong_direction_in_a_batch():
+    for rows, cols in ((48, 300), (160, 220)):
+        g = torch.stack([_strong(rows, cols, 1e-4, s) for s in range(5)])
+        got = binding.orthogonalize_tensor(g).double()
+        for one, o in zip(g, got):
+            want = ref.orthogonalize(one)
+            error, size, rounding = (float(t.norm()) for t in (o - want, want, want.bfloat16().double() - want))
+            assert error <= math.hypot(rounding, 1e-3 * size)
