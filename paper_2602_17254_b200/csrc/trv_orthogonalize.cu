@@ -206,8 +206,8 @@ __device__ __forceinline__ void ns_async16(unsigned to, const void* from) {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
 }
 
-// Loads of the carried operand for columns j .. j + 31 of rows i0 .. i0 + 31
-template <int MODE>
+// Loads of the carried operand for columns j .. j + 31 of rows i0 .. i0 + 31.  FINE: A and B have low halves
+template <int MODE, bool FINE>
 __device__ __forceinline__ void ns_fetch(const NsArgs& a, int z, int i0, int j, unsigned buf) {
     const int lane = threadIdx.x & 31, r = lane >> 2, u = lane & 3;
     if (MODE != NS_GRAM && j < a.N) {
@@ -216,7 +216,7 @@ __device__ __forceinline__ void ns_fetch(const NsArgs& a, int z, int i0, int j, 
         for (int k = 0; k < 4; ++k)
             if (i0 + r + 8 * k < a.M) {
                 ns_async16(ns_unit(buf, r + 8 * k, u), a.hi + at + (size_t)8 * k * a.ld);
-                if (MODE != NS_POLY || a.lo) ns_async16(ns_unit(buf + kNsWarpBuf, r + 8 * k, u), a.lo + at + (size_t)8 * k * a.ld);
+                if (MODE != NS_POLY || FINE) ns_async16(ns_unit(buf + kNsWarpBuf, r + 8 * k, u), a.lo + at + (size_t)8 * k * a.ld);
             }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
@@ -228,18 +228,15 @@ __device__ __forceinline__ unsigned ns_bits(__half2 h) {
     return u;
 }
 
-// a lane's row of 32 values, two to a word, into the transposed image [column][32 rows]
-__device__ __forceinline__ void ns_mirror(unsigned buf, int lane, const unsigned (&row)[16]) {
-    const unsigned to = buf + kNsWarpBuf + lane * 2;
-#pragma unroll
-    for (int k = 0; k < 16; ++k) {
-        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 128 * k), "h"((unsigned short)(row[k] & 0xffff)) : "memory");
-        asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 128 * k + 64), "h"((unsigned short)(row[k] >> 16)) : "memory");
-    }
+// two values of a lane's row, columns 2 k and 2 k + 1, into the transposed image [column][32 rows]
+__device__ __forceinline__ void ns_mirror(unsigned buf, int lane, int k, unsigned pair) {
+    const unsigned to = buf + kNsWarpBuf + 128 * k + lane * 2;
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(to), "h"((unsigned short)(pair & 0xffff)) : "memory");
+    asm volatile("st.shared.b16 [%0], %1;" ::"r"(to + 64), "h"((unsigned short)(pair >> 16)) : "memory");
 }
 
 // get(c, v): the sums of columns c .. c + 31 of this lane's row; cols: a multiple of 32.  ns_fetch has been called for the first 32.
-template <int MODE, typename Get>
+template <int MODE, bool FINE, typename Get>
 __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int j0, int cols, bool mirror, unsigned buf, Get get) {
     const int lane = threadIdx.x & 31, i = i0 + lane;
     const size_t dd = (size_t)z * a.Md;
@@ -250,7 +247,7 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
     for (int c = 0; c < cols; c += 32) {
         const int j = j0 + c;
         if (j >= a.N) break;
-        if (c) ns_fetch<MODE>(a, z, i0, j, buf);
+        if (c) ns_fetch<MODE, FINE>(a, z, i0, j, buf);
         float v[32];
         get(c, v);
         asm volatile("cp.async.wait_group 0;" ::: "memory");
@@ -263,14 +260,16 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 if (i == j + q) on_diag = MODE == NS_GRAM ? a.alpha * v[q] : fmaf(a.alpha, fmaf(d, d, v[q]), a.b * d);
             if (row) a.diag_out[dd + i] = on_diag;
         }
-        unsigned hi[16], low[16];                           // A and B: the row, for the mirror image and the low halves behind the loop
+        // FINE: the row, for the mirror image (its place still holds low halves in the loop) and the low halves behind the loop.  A
+        // kernel of its own: the loop below with the mirror image behind it costs the others 0.3 us a launch.
+        unsigned hi[16], low[16];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const unsigned at = ns_unit(buf, lane, q);
             uint4 u;
             __half2 h[4], l[4];
             if (MODE != NS_GRAM) u = ns_lds(at), memcpy(h, &u, 16);
-            if (MODE >= NS_APPLY || (MODE == NS_POLY && a.lo)) u = ns_lds(at + kNsWarpBuf), memcpy(l, &u, 16);
+            if (MODE >= NS_APPLY || (MODE == NS_POLY && FINE)) u = ns_lds(at + kNsWarpBuf), memcpy(l, &u, 16);
             float4 dj[2];
             if (MODE == NS_POLY) {                          // the same for all lanes; up to the pitch, which is a multiple of 64
                 dj[0] = *(const float4*)(a.diag + dd + j + 8 * q);
@@ -284,7 +283,7 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                     x = f2_mul(x, alpha);
                 } else if (MODE == NS_POLY) {
                     float2 o = __half22float2(h[k]);
-                    if (a.lo) o = f2_fma(__half22float2(l[k]), f2_splat(1.0f / kNsLow), o);
+                    if (FINE) o = f2_fma(__half22float2(l[k]), f2_splat(1.0f / kNsLow), o);
                     const float2 s = k & 1 ? make_float2(dj[k / 2].z, dj[k / 2].w) : make_float2(dj[k / 2].x, dj[k / 2].y);
                     x = f2_fma(alpha, f2_fma(f2_add(d2, s), o, x), f2_mul(b, o));
                 } else {
@@ -301,11 +300,12 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 } else {
                     const __half2 y = __floats2half2_rn(x.x, x.y);
                     hb[k] = ns_bits(y);
-                    if (MODE == NS_APPLY || a.out_lo) {
+                    if (MODE == NS_APPLY || FINE) {
                         const float2 r = f2_mul(f2_fma(__half22float2(y), f2_splat(-1.0f), x), f2_splat(kNsLow));
                         lb[k] = ns_bits(__floats2half2_rn(r.x, r.y));
                     }
-                    if (MODE != NS_APPLY) hi[4 * q + k] = hb[k], low[4 * q + k] = lb[k];
+                    if (FINE) hi[4 * q + k] = hb[k], low[4 * q + k] = lb[k];
+                    else if (MODE != NS_APPLY && mirror) ns_mirror(buf, lane, 4 * q + k, hb[k]);
                 }
             }
             ns_sts(at, make_uint4(hb[0], hb[1], hb[2], hb[3]));
@@ -318,8 +318,9 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
                 if (j + q < a.N) to[q * a.last_col] = __float2bfloat16_rn(v[q]);
         }
         __syncwarp();
-        if (MODE <= NS_POLY && mirror) {
-            ns_mirror(buf, lane, hi);
+        if (FINE && mirror) {
+#pragma unroll
+            for (int k = 0; k < 16; ++k) ns_mirror(buf, lane, k, hi[k]);
             __syncwarp();
         }
         const int r = lane >> 2, u = lane & 3;
@@ -357,11 +358,13 @@ __device__ __forceinline__ void ns_epilogue(const NsArgs& a, int z, int i0, int 
             write(a.out, buf);
             if (MODE == NS_APPLY) write(a.out_lo, buf + kNsWarpBuf);
             if (MODE != NS_APPLY && mirror && i0 < a.M) write_mirror(a.out);
-            if (MODE != NS_APPLY && a.out_lo) {             // the low halves the same way
+            if (FINE) {                                     // the low halves the same way
                 __syncwarp();
 #pragma unroll
                 for (int q = 0; q < 4; ++q) ns_sts(ns_unit(buf, lane, q), make_uint4(low[4 * q], low[4 * q + 1], low[4 * q + 2], low[4 * q + 3]));
-                if (mirror) ns_mirror(buf, lane, low);
+                if (mirror)
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) ns_mirror(buf, lane, k, low[k]);
                 __syncwarp();
                 write(a.out_lo, buf);
                 if (mirror && i0 < a.M) write_mirror(a.out_lo);
@@ -381,7 +384,7 @@ __device__ __forceinline__ void ns_landed(unsigned bar, unsigned n) {
 // right: the same (GRAM, POLY: the product with its transpose) or rows of K, N along x (APPLY, LAST).  Bound by latency: a launch
 // is filling the stages from L2, K / 64 blocks of products, the exchange of a split and one epilogue.  512 x 512: 107 us for 15
 // of these and the two launches before them, 6 to 7 us each.
-template <int MODE>
+template <int MODE, bool FINE>
 __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant__ NsMaps maps,
                                                            const __grid_constant__ NsArgs a, int split) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
@@ -459,11 +462,11 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
         ns_commit<1>(ok ? done : left_off);
         if (!ok) ns_wait(left_off, 0);                      // its products too
     } else {
-        if (cols) ns_fetch<MODE>(a, z, i0 + 32 * q, j0 + first, mine);
+        if (cols) ns_fetch<MODE, FINE>(a, z, i0 + 32 * q, j0 + first, mine);
         ok = __all_sync(~0u, ns_wait(done, 0));
         ns_fence_after();
         if (split == 1 && ok)
-            ns_epilogue<MODE>(a, z, i0 + 32 * q, j0 + first, cols, tj > ti, mine,
+            ns_epilogue<MODE, FINE>(a, z, i0 + 32 * q, j0 + first, cols, tj > ti, mine,
                               [&](int c, float (&v)[32]) { ns_ld32(tmem + ((unsigned)(32 * q) << 16) + first + c, v); });
     }
     if (split > 1) {
@@ -488,7 +491,7 @@ __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant
         ns_cluster_arrive();
         ns_cluster_wait();
         if (warp < kNsEpilogueWarps && cols && ok)
-            ns_epilogue<MODE>(a, z, i0 + 32 * q, j0 + first, cols, tj > ti, mine, [&](int, float (&v)[32]) {
+            ns_epilogue<MODE, FINE>(a, z, i0 + 32 * q, j0 + first, cols, tj > ti, mine, [&](int, float (&v)[32]) {
 #pragma unroll
                 for (int k = 0; k < 32; ++k) v[k] = 0;
 #pragma unroll 1
@@ -544,7 +547,7 @@ __device__ __forceinline__ void ns_tile_at(const NsArgs& a, int t, int* z, int* 
 // the products, whose sums appear in both CTAs' tensor memory, 128 rows each.  5 stages of 32 KB keep the copies ahead of the
 // products; a tile's epilogue runs beside the next tile's products.  4096 x 4096: 59 us for A, 62 for B (half the tiles each), 112
 // for X, the tensor pipe 61 - 65 % busy: 136 tiles of A are 1.8 turns of 74 pairs.
-template <int MODE>
+template <int MODE, bool FINE>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_pair(const __grid_constant__ NsMaps maps,
                                                                                      const __grid_constant__ NsArgs a) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
@@ -644,10 +647,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
             int ti, tj, z;
             ns_tile_at<kSym>(a, n, &z, &ti, &tj);
             const int i0 = ti * 256 + 128 * (int)rank + 32 * q, j0 = tj * 256 + first;
-            ns_fetch<MODE>(a, z, i0, j0, mine);             // while the products run
+            ns_fetch<MODE, FINE>(a, z, i0, j0, mine);             // while the products run
             if (!(ok = __all_sync(~0u, ns_wait(sums(t), tph)))) break;
             ns_fence_after();
-            ns_epilogue<MODE>(a, z, i0, j0, 64, tj > ti, mine, [&](int c, float (&v)[32]) {
+            ns_epilogue<MODE, FINE>(a, z, i0, j0, 64, tj > ti, mine, [&](int c, float (&v)[32]) {
                 ns_ld32(tmem + ((unsigned)(32 * q) << 16) + 256 * t + first + c, v);
             });
             ns_fence_before();                              // the tile after the next may use the buffer
@@ -1174,7 +1177,7 @@ static bool ns_map(CUtensorMap* out, void* base, int inner, int rows, size_t bat
 // instead of 128 4096 x 1024 210 us against 182, up to 74 1024 x 1024 126 us against 123; parts of four blocks instead of eight
 // 1024 x 1024 210 us against 142; one part alone 512 x 2048 154 us against 132 (the last two with slower epilogues).
 constexpr int kNsSplitMax = 128;
-template <int MODE>
+template <int MODE, bool FINE = false>
 static bool ns_product(const NsMaps& maps, NsArgs a, int batch, cudaStream_t st) {
     constexpr bool kSym = MODE == NS_GRAM || MODE == NS_POLY;
     auto count = [&](int t) {
@@ -1194,8 +1197,8 @@ static bool ns_product(const NsMaps& maps, NsArgs a, int batch, cudaStream_t st)
     if (big > kSMs / 4) {
         a.tiles_m = (a.M + 255) / 256, a.tiles_n = (a.N + 255) / 256, a.tiles = (int)big;
         cfg.gridDim = dim3((unsigned)(2 * (big < kSMs / 2 ? big : kSMs / 2)));
-        if (!allow_big_smem_once(k_ns_pair<MODE>, smem, done[0])) return false;
-        e = cudaLaunchKernelEx(&cfg, k_ns_pair<MODE>, maps, a);
+        if (!allow_big_smem_once(k_ns_pair<MODE, FINE>, smem, done[0])) return false;
+        e = cudaLaunchKernelEx(&cfg, k_ns_pair<MODE, FINE>, maps, a);
     } else {
         int split = 1;
         while (split < 4 && small * split * 2 <= kNsSplitMax && a.K / kNsK >= split * 16) split *= 2;
@@ -1203,8 +1206,8 @@ static bool ns_product(const NsMaps& maps, NsArgs a, int batch, cudaStream_t st)
         attr[1].id = cudaLaunchAttributeClusterDimension;
         attr[1].val.clusterDim = {(unsigned)split, 1, 1};
         cfg.numAttrs = 2;
-        if (!allow_big_smem_once(k_ns_tile<MODE>, smem, done[1])) return false;
-        e = cudaLaunchKernelEx(&cfg, k_ns_tile<MODE>, maps, a, split);
+        if (!allow_big_smem_once(k_ns_tile<MODE, FINE>, smem, done[1])) return false;
+        e = cudaLaunchKernelEx(&cfg, k_ns_tile<MODE, FINE>, maps, a, split);
     }
     g_launches.fetch_add(1, std::memory_order_relaxed);
     return e == cudaSuccess;
@@ -1347,7 +1350,8 @@ extern "C" trv_status_t trv_orthogonalize(const void* g, void* out, size_t batch
         apply.last_mat = (long long)out_batch_stride;
         apply.last_vec = !misaligned(out, 16) && out_stride % 8 == 0 && (batch == 1 || out_batch_stride % 8 == 0);
         const NsMaps xx = {xk[p], xk[p], xk[p], xk[p]}, aa = {ak, ak, akl, akl}, bx = {bk, xn[p], bkl, ln[p]};
-        ok = ns_product<NS_GRAM>(xx, gram, (int)batch, st) && ns_product<NS_POLY>(aa, poly, (int)batch, st) &&
+        ok = (L.fine ? ns_product<NS_GRAM, true>(xx, gram, (int)batch, st) && ns_product<NS_POLY, true>(aa, poly, (int)batch, st)
+                     : ns_product<NS_GRAM>(xx, gram, (int)batch, st) && ns_product<NS_POLY>(aa, poly, (int)batch, st)) &&
              (last ? ns_product<NS_LAST>(bx, apply, (int)batch, st) : ns_product<NS_APPLY>(bx, apply, (int)batch, st));
     }
     g_last_kernel = "orthogonalize";

@@ -100,3 +100,13 @@ def test_one_strong_direction_in_a_batch():
             want = ref.orthogonalize(one)
             error, size, rounding = (float(t.norm()) for t in (o - want, want, want.bfloat16().double() - want))
             assert error <= math.hypot(rounding, 1e-3 * size)
+
+
+def test_many_thin_matrices():
+    """So many that CTA pairs take them."""
+    g = torch.stack([_strong(100, 4200, 1e-4, s % 3) if s % 2 else _noise(100, 4200, 1.0, 1e-3, s % 3) for s in range(40)])
+    got = binding.orthogonalize_tensor(g).double()
+    for s in range(40):
+        want = ref.orthogonalize(g[s])
+        error, size, rounding = (float(t.norm()) for t in (got[s] - want, want, want.bfloat16().double() - want))
+        assert error <= math.hypot(rounding, 1e-3 * size)
