@@ -364,8 +364,8 @@ trv_status_t trv_cost_model(trv_plan_t plan, size_t count, size_t elem_size, dou
  * their outputs and workspaces differ.  Matrices are row-major with unit inner stride and a row stride in ELEMENTS; rows may be
  * aligned to their element size only (16-byte aligned rows of equal 16-byte offsets are faster).  A size of zero is no error.
  * Outputs and workspaces must not overlap inputs or one another (INVALID_ARG); column slices of one buffer that share no element
- * are fine.  Sums, statistics and softmaxes are binary32 or
- * wider; every result is rounded once, to the type of its buffer, and is the same from run to run (no floating atomics).
+ * are fine.  Sums, statistics and softmaxes are binary32 or wider; every result is rounded once, to the type of its buffer, and is
+ * the same from run to run (no floating atomics).
  * workspace: DEVICE, 256-byte aligned, at least the bytes the query names (SCRATCH otherwise); contents undefined before and after.
  *
  * Layer norm over the last dimension: per row of `cols` values mu = mean, r = 1 / sqrt(variance + eps) (biased variance),
@@ -394,6 +394,8 @@ trv_status_t trv_layernorm_workspace_bytes(size_t rows, size_t cols, size_t *byt
  *   gates    : DEVICE float32 [tokens][top_k]: p at the ids (0 at -1); normalize != 0 divides by their sum
  *   counts   : DEVICE int32 [experts + 1]: tokens that chose each expert, and last the number N of tokens not left out
  *   prob_sum : DEVICE float32 [experts]: sum of p over the tokens not left out
+ * Probabilities are binary32, off by up to (2.3 d + E / 32 + 20) 2^-24 of themselves for a logit d below the token's largest among E;
+ * those below 2^-126 are 0.
  * counts and prob_sum of several ranks are summed by an INT32 and a FLOAT32 AllReduce before they enter the next two calls.
  * Limits (UNSUPPORTED): 1024 experts, top_k 32, 2^31 - 1 tokens. */
 trv_status_t trv_router_forward(const void *logits, const uint8_t *mask, int32_t *ids, float *gates, int32_t *counts, float *prob_sum,
@@ -429,7 +431,8 @@ trv_status_t trv_router_backward(const void *logits, const uint8_t *mask, const 
  *                  The order of the sums goes by the sizes, the batch included
  *   coefficients : HOST float [steps][3] = (a, b, c) of every step, NULL: 3.4445, -4.7750, 2.0315 in all.  A and a I + b A + c A A must
  *                  stay below 255 in magnitude (singular values stay below about 1.3 with the default), else the result is infinite or NaN
- * A zero matrix gives zeros.  Limits: steps 1 .. 64 (INVALID_ARG), rows and cols 2^20, batch 65535 (UNSUPPORTED).
+ * A zero matrix gives zeros.  Matrices with a side of at most 128 run in clusters of up to 16 CTAs: a partition of a GPU that cannot
+ * hold such a cluster gets CUDA.  Limits: steps 1 .. 64 (INVALID_ARG), rows and cols 2^20, batch 65535 (UNSUPPORTED).
  * The first call on a device looks up a device address and the tensor-map encoder: make it outside any stream capture.
  * Bounded waits as in the other copy-engine kernels: see trv_tma_giveups. */
 trv_status_t trv_orthogonalize(const void *g, void *out, size_t batch, size_t rows, size_t cols, size_t g_stride, size_t g_batch_stride,

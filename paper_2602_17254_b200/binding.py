@@ -413,6 +413,9 @@ def allreduce_tensor(plan, x, out=None, kernel=KERNEL_AUTO, global_count=None, g
     return dst
 
 
+# Tensor forms of the training operators.  They stand outside autograd, as the AllReduce does: results carry no gradient function even if an
+# input requires gradients, and the backward forms are calls of their own (the forward and backward of a torch.autograd.Function, say).
+
 _FLOAT_CODES = {}       # torch dtype -> type code of the training operators; filled on first use
 
 
@@ -491,7 +494,8 @@ def _workspace(need, workspace, like):
 
 
 def layernorm_forward_tensor(x, gamma=None, beta=None, eps=1e-5, out=None):
-    """Layer norm of the rows of a CUDA matrix: (y, mean, rstd); mean and rstd (float32) are for the backward pass."""
+    """Layer norm of the rows of a CUDA matrix: (y, mean, rstd); mean and rstd (float32) are for the backward pass.
+    Outside autograd: layernorm_backward_tensor is the gradient."""
     rows, cols, xs = _matrix(x, "x")
     device, stream = _stream_of(x)
     ptype, pcode = _param_type(x, beta if gamma is None else gamma)
@@ -534,7 +538,8 @@ def _token_mask(mask, tokens, device):
 
 
 def router_forward_tensor(logits, top_k, mask=None, normalize=True, workspace=None):
-    """(ids, gates, counts, prob_sum) of a CUDA matrix of logits [tokens, experts]; see trv_router_forward."""
+    """(ids, gates, counts, prob_sum) of a CUDA matrix of logits [tokens, experts]; see trv_router_forward.
+    Outside autograd: router_backward_tensor is the gradient."""
     tokens, experts, ls = _matrix(logits, "logits")
     device, stream = _stream_of(logits)
     i32, f32 = _torch.int32, _torch.float32

@@ -12,7 +12,12 @@
 // the row, packing; hence the packed binary32 arithmetic, and forward as many elements a thread as registers allow, since a row's
 // sums cost every thread the same; backward the parameters' gradients take the registers).  Measured:
 // forward 16384 x 4096 bfloat16 45 us, 6.0 TB/s, 32768 x 8192 168 us, 6.4 TB/s; backward 32768 x 8192 bfloat16 288 us, 5.6 TB/s;
-// 6561 x 2187 float32, rows that start off 16-byte boundaries, forward 24.5 us, 4.7 TB/s, backward 37 us, 4.6 TB/s.
+// 6561 x 2187 float32, rows that start off 16-byte boundaries, forward 24.5 us, 4.7 TB/s, backward 37 us, 4.6 TB/s.  Further from
+// memory's rate: short rows (65536 x 512 bfloat16 backward 43 us, 200000 x 100 float32 33 us forward, 52 backward: 80 - 127 registers,
+// 2 to 3 CTAs of a warp per row); rows off 16-byte boundaries (122 - 146 registers, 1 or 2 CTAs per SM); pairs of CTAs (8192 x 16384
+// bfloat16 backward 220 us: a cluster barrier per row with nothing to do meanwhile).  Operands that start at different places of a
+// 16-byte vector are read element by element, nothing ahead; so are rows above 16384 columns, in three passes.  Spills: pairs with loose
+// ends 32 (16-bit) and 64 bytes (float32), forward float32 rows above 8192 columns with loose ends 60.
 #include <atomic>
 
 #include "trv_train.cuh"

@@ -402,8 +402,8 @@ __global__ void __launch_bounds__(kRtThreads) k_balance_loss(const int* __restri
 }
 
 // The gates' gradients reach their experts' lanes through a row of shared memory per token, zero but for the chosen places.  Four CTAs
-// per SM where 64 registers do without spilling: 65536 x 64 12.5 -> 11.9 us; below 8 lanes to a token they spill, 131072 x 16 float32
-// 13.0 -> 14.4 us.
+// per SM (64 registers) from 8 lanes to a token on, although that spills 80 to 104 bytes with 8 lanes and 16 with 16 of them:
+// 65536 x 64 12.5 -> 11.9 us; with fewer lanes it does not pay, 131072 x 16 float32 13.0 -> 14.4 us.
 template <typename T, int V, int G>
 __global__ void __launch_bounds__(kRtThreads, V == 8 && G >= 8 ? 4 : 1) k_router_bwd(const RouterArgs<T> a) {
     constexpr int PER = 32 / G, KMAX = V * G < kRtMaxK ? V * G : kRtMaxK, TURNS = (KMAX + G - 1) / G;     // choices of a token: TURNS per lane
