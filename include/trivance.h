@@ -423,11 +423,12 @@ trv_status_t trv_router_backward(const void *logits, const uint8_t *mask, const 
  *   g            : DEVICE [batch][rows][cols] of dtype (FLOAT32, BFLOAT16, FLOAT16); strides in elements (rows, matrices)
  *   out          : DEVICE BFLOAT16, same shape, strides of its own; its matrices must not overlap.  Products of binary16
  *                  operands with binary32 sums.  With one side of at most 128 and the other of at most 4096 operands have two binary16
- *                  halves: within 0.05 % (2-norm) of the exact result before its rounding to BFLOAT16 (0.17 %), for every spectrum.
+ *                  halves: within 0.1 % (2-norm, mostly 0.01 %) of the exact result before its rounding to BFLOAT16 (0.17 %), for every
+ *                  spectrum.
  *                  Else one half (diagonals, the carried term and what would still grow in more bits): with the default coefficients
  *                  within 0.1 % for noise and for strong directions over weak ones, 0.4 % where all entries are of one magnitude, so
- *                  that their roundings agree; steep coefficients amplify the roundings: 8.287, -23.60, 17.30 and the four that
- *                  go with them to 0.5 % (1.2 % with a side below 129).
+ *                  that their roundings agree; steep coefficients amplify the roundings, to 0.5 % (1.2 % with a side below 129) in
+ *                  steps that start with 8.287, -23.60, 17.30, whose slopes reach 12 where singular values pass.
  *                  The order of the sums goes by the sizes, the batch included
  *   coefficients : HOST float [steps][3] = (a, b, c) of every step, NULL: 3.4445, -4.7750, 2.0315 in all.  A and a I + b A + c A A must
  *                  stay below 255 in magnitude (singular values stay below about 1.3 with the default), else the result is infinite or NaN

@@ -6,8 +6,8 @@
 // Number formats.  A gradient has a few strong directions and many weak ones; the weak ones grow by a factor of up to a in every
 // step, and so does every rounding of the strong ones that falls on them.  So X is held as hi + lo, two binary16 numbers (22 bits).
 // On chip (k_ns_small: a side of at most 128, the other up to 4096) all three products take both halves of both operands, hi lo +
-// lo hi + hi hi; B includes a I.  The result is then within 0.05 % of the 64-bit one for every spectrum and for steep
-// coefficients, 0.01 % mostly.
+// lo hi + hi hi; B includes a I.  The result is then within 0.05 % of the 64-bit one for every spectrum measured
+// and for steep coefficients, 0.01 % mostly.
 // In the tiled kernels hi is the operand and the carried term a X uses both.  A and B are nearly diagonal once the singular
 // values are near 1, so their diagonals are kept apart, in binary32, and only the rest is rounded to binary16:
 //     A = D + O,  B = E + P:  P = b O + c (O O + (D_i + D_j) O) off the diagonal, E = b D + c (O O + D D) on it,
@@ -25,8 +25,8 @@
 // buffered in tensor memory, so that one tile is written while the next is computed.  Matrices with a side of 128 or less stay on
 // chip for all steps (k_ns_small).  A step is work of 3 M M N + M M M operations (of the symmetric A and B only half the tiles are
 // computed, the others are their mirror images).  Measured, 5 steps: 8192 x 8192 float32 9.4 ms, 1.17 PFLOP/s, bound by the tensor
-// cores under the power limit; 4096 x 4096 1.16 ms, 1.18 PFLOP/s; 4096 x 1024 181 us, 0.39 PFLOP/s, bound by 17 dependent launches
-// of 36 to 256 tiles.
+// cores under the power limit; 4096 x 4096 1.16 - 1.19 ms, 1.17 PFLOP/s; 4096 x 1024 187 us, 0.37 PFLOP/s, bound by 17 dependent
+// launches of 36 to 256 tiles and, in A, by the operands' way through L2 (75 MB).
 #include "trv_tma.cuh"
 #include "trv_train.cuh"
 
@@ -382,7 +382,7 @@ __device__ __forceinline__ void ns_landed(unsigned bar, unsigned n) {
 
 // One 128 x 128 tile of  left . right  per cluster, the sum over K split over its CTAs.  left: rows along y, K along x.
 // right: the same (GRAM, POLY: the product with its transpose) or rows of K, N along x (APPLY, LAST).  Bound by latency: a launch
-// is filling the stages from L2, K / 64 blocks of products, the exchange of a split and one epilogue.  512 x 512: 107 us for 15
+// is filling the stages from L2, K / 64 blocks of products, the exchange of a split and one epilogue.  512 x 512: 111 us for 15
 // of these and the two launches before them, 6 to 7 us each.
 template <int MODE, bool FINE>
 __global__ void __launch_bounds__(kNsThreads, 1) k_ns_tile(const __grid_constant__ NsMaps maps,
@@ -676,7 +676,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kNsThreads, 1) k_ns_
 // 128-byte-swizzled layout serves as K-major operand of X X^T and as N-major operand of B X; A and B are there too.  A step is
 // three products (three times: see the header) and three passes over registers, 16 columns of a row per thread and turn; a cluster
 // adds the CTAs' parts of X X^T through distributed shared memory, every CTA a share of the columns, in a fixed order.  Bound by the
-// latency of this chain: 81 x 243 float32 43 us, 32 matrices of 128 x 1000 94 us, 16 x 40 16 us (with high halves alone 31, 61
+// latency of this chain: 81 x 243 float32 44 us, 32 matrices of 128 x 1000 91 us, 16 x 40 16 us (with high halves alone 31, 61
 // and 14 us and errors of up to 3 %: 2/3 of the difference are the additional products, the rest of a cluster's the doubled exchange of A).
 // Sides are rounded up to 16, not to 128: 16 x 40 took 24 us with 128.  The code is kept small (loops of 16 columns, one pass for
 // every purpose): run once by a CTA it comes from memory, and unrolled loads of 128 elements a thread took 20 us for their
@@ -1129,8 +1129,8 @@ __global__ void __launch_bounds__(256) k_ns_prepare(const T* __restrict__ g, int
 }
 
 // Tiled kernels: up to this M the square matrices have low halves too.  That takes the roundings of P away, which fall on few rows
-// there (16 x 8192, one direction over 1e-5: 0.12 -> 0.004 %, 3 x 9000, a level over noise 0.10 -> 0.04 %), for 104 -> 119 us at
-// 16 x 8192; 200 x 300 would go from 117 to 143 us and from 0.08 to 0.06 %.
+// there (16 x 8192, one direction over 1e-5: 0.12 -> 0.004 %, 3 x 9000, a level over noise 0.10 -> 0.04 %), for a tenth more time;
+// 200 x 300 would go from 0.08 to 0.06 % and take a quarter more.
 constexpr int kNsFine = 128;
 struct NsLayout {
     int M, N, ldm, ldn, parts;

@@ -92,6 +92,14 @@ def test_steep_steps_tiled(rows, cols):
     _check(_strong(rows, cols, 1e-3), 7.5e-3, STEEP)
 
 
+def test_a_thousandth_at_300_by_1000():
+    for seed in (0, 1):
+        for weak in (1e-3, 1e-4):
+            _check(_strong(300, 1000, weak, seed), 1e-3)
+        _check(_noise(300, 1000, 1.0, 1e-3, seed), 1e-3)
+        _check(_noise(300, 1000, seed=seed), 1e-3, STEEP)
+
+
 def test_one_strong_direction_in_a_batch():
     for rows, cols in ((48, 300), (160, 220)):
         g = torch.stack([_strong(rows, cols, 1e-4, s) for s in range(5)])
